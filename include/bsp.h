@@ -169,6 +169,50 @@ int bsp_adam_step(float *W, const void *G, int gdt, float *m, float *v, int64_t 
                   const float *alpha, float lambda, int mode, const uint8_t *keep, float lr, float beta1,
                   float beta2, float eps, int64_t t, void *stream);
 
+/* ---- one weight update of all tensors of a model (Alg. 2's "update W ... using Adam" for whole networks, with
+ * decoupled weight decay) ------------------------------------------------------------------------
+ * For every element of every tensor, fp32, one rounding per operation; g in gdt, the master weights w fp32:
+ *   g <- grad_scale * g           if grad_scale != NULL (a device float, read by the kernels: a clipping factor; where
+ *                                 it is not finite the whole step is skipped and every buffer keeps its bits)
+ *   g <- fma(lambda * alpha, w, g) if the tensor has alpha: Eq. 3 with fixed factors, squared-norm form (bsp_adam_step)
+ *   m <- beta1*m + (1-beta1)*g;   v <- beta2*v + ((1-beta2)*g)*g
+ *   w <- w - (lr*weight_decay)*w  where that is not 0
+ *   w <- w - (lr*(m/c1)) / (sqrt(v/c2) + eps),  c = 1 - beta^t
+ *   w <- +0                       if the tensor has keep and keep[b][j] == 0
+ *   copy <- w in cdt (RNE)        if the tensor has a copy: the 16-bit weights of the next forward pass
+ * state_bits 32: m and v are fp32 tensors; without decay, copy and grad_scale the bits are those of bsp_adam_step.
+ * state_bits 8: m and v are e4m3 codes (4 exponent and 3 mantissa bits, no infinity), v of r = sqrt(v); for every 256
+ *   consecutive elements (the last block of a tensor may be shorter) scales holds the largest |m|, then, ceil(M N / 256)
+ *   floats further on, the largest r, each divided by 448: a moment is its code times its block's scale.  A new moment goes to
+ *   one of its two neighbouring codes at random, in proportion to its distance, with 16 bits each for m and r mixed from the
+ *   element's index in its tensor, t and seed: equal calls give equal bits.  r > 0 is stored as the least positive code at
+ *   least; a block whose largest value is below 2^-100 as zeros.  The update itself uses the moments before they are
+ *   stored.  All-zero codes and scales are a fresh state.
+ * tensors: HOST array of `count` descriptions, read during the call; device pointers in it.  Tensors are [M, N] row-major and
+ *   contiguous (a vector: M = 1), of any size, 0 included; keep and alpha are [M / R, N], R is read only with them.
+ *   No two tensors of a call may overlap (weights that do, a tied tensor listed twice, are refused).  Addresses need
+ *   their element's alignment.
+ * lr_t: NULL, or two device floats {lr, t} that the kernels read in the place of the arguments: a step that was captured in
+ *   a graph is replayed with new ones (t as a float: exact up to 2^24).
+ * Up to 40 tensors are one launch.  Errors: BSP_ERR_NULL, BSP_ERR_DTYPE (gdt; cdt other than bf16 / fp16),
+ * BSP_ERR_SHAPE (state_bits, t < 1 without lr_t, negative sizes, N >= 2^31, M % R != 0 with keep or alpha, misalignment,
+ * weights that overlap), BSP_ERR_CAPACITY (no host memory for that check). */
+typedef struct {
+    float *w;
+    const void *g;
+    void *m, *v;
+    float *scales;       /* 2 * ceil(M N / 256) floats (state_bits 8), else unused */
+    void *copy;          /* may be NULL */
+    const uint8_t *keep; /* may be NULL */
+    const float *alpha;  /* may be NULL */
+    int64_t M, N;
+    int32_t R;
+    float weight_decay;
+} bsp_adamw_tensor;
+int bsp_adamw_step(const bsp_adamw_tensor *tensors, int64_t count, int gdt, int cdt, int state_bits, float lambda, float lr,
+                   float beta1, float beta2, float eps, int64_t t, uint32_t seed, const float *lr_t, const float *grad_scale,
+                   void *stream);
+
 /* ---- compact storage (Sec. 3.1: only the kept columns of a block are indexed) ----------
  * Layout.  For block b: cols_b = ascending j with keep[b, j] != 0; k_b = |cols_b| =
  * blk_cnt[b]; kp_b = k_b rounded up to a multiple of k_align (0 stays 0);
@@ -358,6 +402,79 @@ int bsp_linear_planned(const void *X, int xdt, int64_t T, int64_t M, int64_t N, 
 int bsp_linear_planned_fused(const void *X, int xdt, int64_t T, int64_t M, int64_t N, int32_t R, int32_t k_align,
                              const void *plan, int64_t capacity_cols, const void *bias, int act,
                              const void *residual, void *Y, void *stream);
+
+/* ---- the norms round a block (Sec. 4.2: the networks' blocks are joined by a residual addition and a norm) ---------------
+ * Between the pruned layers of one block and those of the next:
+ *   n = N_post(F)                      (BSP_NORM_POST; else n = F)
+ *   Z = round(x_scale * X + gate * n)  H = round(N_pre(Z))  (BSP_NORM_PRE; else no H)
+ *   N(v) = (v - mean) * rstd * w + b,  rstd = 1 / sqrt(mean((v - mean)^2) + eps);  BSP_NORM_RMS: mean = 0
+ * BERT's form is norms = BSP_NORM_PRE, x_scale = 1, no gate: Z the sum, H what the next block reads and adds to.  All
+ * arithmetic and sums are fp32; N_pre reads Z as it was rounded, whether or not it is written.
+ * X, F, Z, H: [T, H] row-major of type dt, H <= 8192; F may be NULL (Z = x_scale X) without BSP_NORM_POST and gate; Z may be
+ * NULL with BSP_NORM_PRE.  w_*, b_*: [H] of type dt, each may be NULL (1 and 0).  gate: [gate_rows, H] of type dt or NULL;
+ * row i of it is for rows i T / gate_rows onwards (gate_rows divides T): 1 a gate per channel, the batch one per sequence, T
+ * one per token.  stats_*: [T, 2] fp32 or NULL, mean and rstd of every row, which the backward pass takes.
+ * Z and H may be X or F (in place); other overlaps are not allowed.
+ *
+ * bsp_block_norm_backward: the gradients for dZ (NULL: zero) and dH of one loss; with d = dZ + the gradient through N_pre,
+ *   dX = x_scale * d,  dF = gradient through gate and N_post of d,  each written where it is not NULL, in dt;
+ *   dw_*, db_* [H] and dgate [gate_rows, H] fp32, each may be NULL, summed over the rows in a fixed order: two calls with
+ *   the same arguments give the same bits.  Arguments as in the forward call, Z as it wrote it; X is not needed, F for
+ *   BSP_NORM_POST and dgate only, dH, Z and stats_pre for BSP_NORM_PRE only.  dX and dF may be dZ or dH (not each other).
+ * ws: bsp_block_norm_backward_workspace_bytes(T, H, gate_rows) bytes (gate_rows 0 without a gate), 256-byte aligned,
+ *   undefined before and after; calls that may overlap need one each.  Only needed where a sum down the rows is asked for.
+ * T == 0: nothing, and sums of zero.  Errors: BSP_ERR_NULL, BSP_ERR_DTYPE (dt, kind, norms), BSP_ERR_SHAPE (H outside 1 ..
+ * 8192, T >= 2^31, gate_rows, a gradient of what is absent, misalignment), BSP_ERR_CAPACITY (ws_bytes). */
+typedef enum { BSP_NORM_LAYER = 0, BSP_NORM_RMS = 1 } bsp_norm_kind;
+typedef enum { BSP_NORM_POST = 1, BSP_NORM_PRE = 2 } bsp_norm_place;
+int bsp_block_norm(const void *X, const void *F, int dt, int64_t T, int64_t H, int norms, int kind, float eps, float x_scale,
+                   const void *gate, int64_t gate_rows, const void *w_post, const void *b_post, const void *w_pre,
+                   const void *b_pre, void *Z, void *Hn, float *stats_post, float *stats_pre, void *stream);
+size_t bsp_block_norm_backward_workspace_bytes(int64_t T, int64_t H, int64_t gate_rows);
+int bsp_block_norm_backward(const void *dZ, const void *dH, const void *Z, const void *F, int dt, int64_t T, int64_t H, int norms,
+                            int kind, float x_scale, const void *gate, int64_t gate_rows, const void *w_post,
+                            const void *b_post, const void *w_pre, const float *stats_post, const float *stats_pre, void *dX,
+                            void *dF, float *dw_post, float *db_post, float *dw_pre, float *db_pre, float *dgate, void *ws,
+                            size_t ws_bytes, void *stream);
+
+/* ---- products in 8-bit floating point (the layer of Sec. 3.1 and its gradients on the masked dense matrix, at twice
+ * the rate of the 16-bit matrix instructions) ------------------------------------------------------
+ * A quantised matrix is codes of e4m3 (4 exponent and 3 mantissa bits, largest value 448, no infinity), row-major with rows
+ * of cp = cols rounded up to a multiple of 128 bytes, and scales: biased exponents of powers of two, one byte each (value
+ * 2^(s - 127)).  BSP_FP8_ROW: a scale per 128 columns of a row, [rows, cp / 128]; BSP_FP8_BLOCK: per 128 x 128 block,
+ * [ceil(rows / 128), cp / 128].  A value is its code times its scale; columns past cols hold code 0.
+ *
+ * bsp_fp8_quant: X [rows, cols] of xdt -> Q, S (codes and scales) and / or Qt, St: those of the transposed matrix, [cols, rp]
+ * with segments along X's rows (BSP_FP8_ROW) or the same blocks (BSP_FP8_BLOCK).  The scale is the least power of two that
+ * brings the segment's largest finite magnitude to 448 or below (2^0 for zeros, never below 2^-127); the code is the nearest
+ * (ties to even).  What is not finite becomes NaN.  Q or Qt may be NULL; both 16-byte aligned.
+ *
+ * bsp_matmul_fp8: Y = round(act(A B^T + bias) + residual) for quantised A [T, K] (BSP_FP8_ROW) and B [M, K] (b_layout):
+ *   the layer          A = X,               B = W  (M x N, usually BSP_FP8_BLOCK)
+ *   input gradient     A = dY,              B = the transposed W of the same call of bsp_fp8_quant
+ *   weight gradient    A = dY transposed,   B = X transposed (both BSP_FP8_ROW: segments along the tokens), ydt = BSP_F32
+ * The matrix cores' sums are fp32, scaled exactly, and rounded once to ydt.  For 16-bit results the instruction on 8-bit codes is
+ * used, which drops what lies 14 binades below the largest product of the few it adds at once (1.3e-5 of the result); for fp32
+ * results one with exact products, at half the rate. bias [M] and
+ * residual [T, M] have type ydt and may be NULL, act is a bsp_activation.  Y: [T, M].  The order of the additions is fixed for
+ * given arguments: two calls give the same bits.  Codes past K must be 0 in A and B (bsp_fp8_quant's are).
+ * ws: scratch for products of few outputs and many columns, bsp_matmul_fp8_workspace_bytes(T, M, K) bytes (may be 0), 256-byte
+ * aligned, undefined before and after; with NULL the call does without, slower.
+ *
+ * bsp_linear_fp8: the layer on X [T, N] of type xdt and quantised W [M, N]: bsp_fp8_quant of X and bsp_matmul_fp8 in one call,
+ * the same bits; bias, residual and Y have type xdt.  ws: bsp_linear_fp8_workspace_bytes(T, M, N) bytes, 256-byte aligned.
+ *
+ * rows, T may be 0 (nothing is done); K <= 2^23.  Errors: BSP_ERR_NULL, BSP_ERR_DTYPE (types, layout, act), BSP_ERR_SHAPE (sizes,
+ * A, B, Q, Qt not 16-byte aligned, others not by their element), BSP_ERR_CAPACITY (ws_bytes too small). */
+typedef enum { BSP_FP8_ROW = 0, BSP_FP8_BLOCK = 1 } bsp_fp8_layout;
+int bsp_fp8_quant(const void *X, int xdt, int64_t rows, int64_t cols, int layout, void *Q, uint8_t *S, void *Qt, uint8_t *St,
+                  void *stream);
+size_t bsp_matmul_fp8_workspace_bytes(int64_t T, int64_t M, int64_t K);
+int bsp_matmul_fp8(const void *A, const uint8_t *SA, const void *B, const uint8_t *SB, int b_layout, int64_t T, int64_t M, int64_t K,
+                   const void *bias, int act, const void *residual, void *Y, int ydt, void *ws, size_t ws_bytes, void *stream);
+size_t bsp_linear_fp8_workspace_bytes(int64_t T, int64_t M, int64_t N);
+int bsp_linear_fp8(const void *X, int xdt, int64_t T, int64_t M, int64_t N, const void *W, const uint8_t *SW, int w_layout,
+                   const void *bias, int act, const void *residual, void *Y, void *ws, size_t ws_bytes, void *stream);
 
 /* ---- helpers (host only) -------------------------------------------------------------- */
 /* dense parameters / kept parameters = M*N / (R * kept_cols_total) (Sec. 4.4: 1.428x <=> 30 % sparsity) */

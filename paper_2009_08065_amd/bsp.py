@@ -21,7 +21,7 @@ _TORCH = {F32: torch.float32, BF16: torch.bfloat16, F16: torch.float16}
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
 _NATIVE = None
-_U8, _I32 = 3, 4  # types of a native allocation that are none of the library's
+_U8, _I32, _E4M3 = 3, 4, 5  # types of a native allocation that are none of the library's
 
 
 class BspError(RuntimeError):
@@ -91,6 +91,19 @@ def lib():
     L.bsp_linear_plan.argtypes = [C.c_int, i64, i64, i32, i32, vp, vp, vp, vp, i64, vp, sz, vp]
     L.bsp_linear_planned.argtypes = [vp, C.c_int, i64, i64, i64, i32, i32, vp, i64, vp, vp, vp]
     L.bsp_linear_planned_fused.argtypes = [vp, C.c_int, i64, i64, i64, i32, i32, vp, i64, vp, C.c_int, vp, vp, vp]
+    L.bsp_fp8_quant.argtypes = [vp, C.c_int, i64, i64, C.c_int, vp, vp, vp, vp, vp]
+    L.bsp_matmul_fp8_workspace_bytes.argtypes = [i64, i64, i64]
+    L.bsp_matmul_fp8_workspace_bytes.restype = sz
+    L.bsp_matmul_fp8.argtypes = [vp, vp, vp, vp, C.c_int, i64, i64, i64, vp, C.c_int, vp, vp, C.c_int, vp, sz, vp]
+    L.bsp_linear_fp8_workspace_bytes.argtypes = [i64, i64, i64]
+    L.bsp_linear_fp8_workspace_bytes.restype = sz
+    L.bsp_linear_fp8.argtypes = [vp, C.c_int, i64, i64, i64, vp, vp, C.c_int, vp, C.c_int, vp, vp, vp, sz, vp]
+    L.bsp_block_norm.argtypes = [vp, vp, C.c_int, i64, i64, C.c_int, C.c_int, f32, f32, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.bsp_block_norm_backward_workspace_bytes.argtypes = [i64, i64, i64]
+    L.bsp_block_norm_backward_workspace_bytes.restype = sz
+    L.bsp_block_norm_backward.argtypes = [vp, vp, vp, vp, C.c_int, i64, i64, C.c_int, C.c_int, f32, vp, i64, vp, vp, vp, vp, vp,
+                                          vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.bsp_adamw_step.argtypes = [vp, i64, C.c_int, C.c_int, C.c_int, f32, f32, f32, f32, f32, i64, C.c_uint32, vp, vp, vp]
     L.bsp_compression_rate.argtypes = [i64, i64, i32, i64]
     L.bsp_compression_rate.restype = C.c_double
     L.bsp_status_string.argtypes = [C.c_int]
@@ -100,7 +113,8 @@ def lib():
     for name in ("bsp_group_norms", "bsp_penalty_grad", "bsp_prune_mask", "bsp_pack_count", "bsp_pack",
                  "bsp_packed_validate", "bsp_linear", "bsp_linear_ws", "bsp_linear_sized", "bsp_linear_transposed", "bsp_linear_transposed_ws", "bsp_linear_transposed_dense", "bsp_linear_dvals", "bsp_linear_plan", "bsp_linear_planned", "bsp_linear_planned_fused",
                  "bsp_mask_weights",
-                 "bsp_group_norms_grad", "bsp_adam_step", "bsp_prune_mask_count"):
+                 "bsp_group_norms_grad", "bsp_adam_step", "bsp_prune_mask_count", "bsp_fp8_quant", "bsp_matmul_fp8", "bsp_linear_fp8", "bsp_block_norm",
+                 "bsp_block_norm_backward", "bsp_adamw_step"):
         getattr(L, name).restype = C.c_int
     _LIB = L
     return L
@@ -133,6 +147,14 @@ def _stream():
     """The current stream of the current device as an integer.  (torch.cuda.current_stream() builds a Stream object for
     it: 2.8 of the 9.9 us that a call of bsp_linear_planned took on the host; this takes 0.1.)"""
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
+def _here(*tensors):
+    """The kernels go to the current device's stream: tensors of another one are refused."""
+    device = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"tensors must be on the current device ({device}), got one on {t.device}")
 
 
 def _scratch(need: int, device):
@@ -205,6 +227,31 @@ def bsp_adam_step(W, G, m, v, R, lr, beta1=0.9, beta2=0.999, eps=1e-8, t=1, alph
     st = native.bsp_adam_step(W, G, _DT[G.dtype], m, v, M, N, R, alpha, lam, mode, keep, lr, beta1,
                               beta2, eps, t, _stream())
     _check(st, "bsp_adam_step")
+    return W, m, v
+
+
+def bsp_adamw_state(W, bits=32):
+    """Fresh moments for bsp_adamw_step of the tensors W: lists (m, v, scales), scales None for 32 bits."""
+    if bits == 32:
+        return [torch.zeros_like(w, dtype=torch.float32) for w in W], [torch.zeros_like(w, dtype=torch.float32) for w in W], None
+    if bits != 8:
+        raise ValueError("moments are held in 32 or 8 bits")
+    code = lambda w: torch.zeros(w.shape, dtype=torch.uint8, device=w.device).view(torch.float8_e4m3fn)
+    return ([code(w) for w in W], [code(w) for w in W],
+            [torch.zeros((2, (w.numel() + 255) // 256), dtype=torch.float32, device=w.device) for w in W])
+
+
+def bsp_adamw_step(W, G, m, v, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, t=1, scales=None, keep=None, alpha=None,
+                   lam=0.0, R=16, copies=None, seed=0, lr_t=None, grad_scale=None):
+    """One Adam step with decoupled weight decay over lists of tensors, in place: fp32 weights W, gradients G of one dtype, moments
+    m and v (fp32, or e4m3 with scales: bsp_adamw_state).  keep, alpha, copies: lists whose entries may be None (masks and
+    Eq. 3 factors [M / R, N] of a matrix [M, N], 16-bit copies of the new weights); weight_decay, R: numbers or lists.
+    lr_t: device tensor {lr, t} read in the place of the arguments; grad_scale: device tensor of one."""
+    native = _native()
+    bits = 32 if scales is None else 8
+    st = native.bsp_adamw_step(W, G, m, v, scales, copies, keep, alpha, R, weight_decay, bits, lam, lr, beta1, beta2, eps, t, seed,
+                               lr_t, grad_scale, torch._C._cuda_getDevice(), _stream())
+    _check(st, "bsp_adamw_step")
     return W, m, v
 
 
@@ -512,6 +559,167 @@ def bsp_linear_planned_fused(X, p: Packed, plan, bias=None, act=ACT_NONE, residu
                                          p.total_cols, bias, act, residual, Y, _stream())
     _check(st, "bsp_linear_planned_fused")
     return Y
+
+
+FP8_ROW, FP8_BLOCK = 0, 1
+
+
+@dataclass
+class Fp8:
+    """A matrix [rows, cols] in 8-bit floating point: e4m3 codes [rows, cols up to a multiple of 128] and biased exponents of its
+    scales (uint8), one per 128 columns of a row (FP8_ROW) or per 128 x 128 block (FP8_BLOCK)."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    rows: int
+    cols: int
+    layout: int
+
+
+def _fp8_fits(q: Fp8):
+    steps = (q.cols + 127) // 128
+    lines = q.rows if q.layout == FP8_ROW else (q.rows + 127) // 128
+    if q.codes.dtype != torch.float8_e4m3fn or q.codes.numel() != q.rows * steps * 128 or q.scales.numel() != lines * steps:
+        raise ValueError("codes (float8_e4m3fn) and scales do not have the sizes of their matrix")
+
+
+def bsp_fp8_quant(X, layout=FP8_ROW, want=("plain",)):
+    """X [rows, cols] in 8 bits: (Fp8 of X, Fp8 of the transposed X), the ones not in `want` ("plain", "transposed") None."""
+    native = _native()
+    _here(X)
+    rows, cols = X.shape
+    made = []
+    for name, r, c in (("plain", rows, cols), ("transposed", cols, rows)):
+        if name not in want:
+            made.append(None)
+            continue
+        steps = (c + 127) // 128
+        lines = r if layout == FP8_ROW else (r + 127) // 128
+        made.append(Fp8(native.empty(X, _E4M3, r, steps * 128), native.empty(X, _U8, lines, steps), r, c, layout))
+    p, t = made
+    st = native.bsp_fp8_quant(X, _DT[X.dtype], rows, cols, layout, p and p.codes, p and p.scales, t and t.codes, t and t.scales, _stream())
+    _check(st, "bsp_fp8_quant")
+    return p, t
+
+
+def _epilogue_fits(T, M, dtype, bias, residual):
+    if bias is not None and (bias.dtype != dtype or bias.numel() != M):
+        raise ValueError("bias must have M elements of the dtype of the result")
+    if residual is not None and (residual.dtype != dtype or tuple(residual.shape) != (T, M)):
+        raise ValueError("residual must be a [T, M] tensor of the dtype of the result")
+
+
+def bsp_matmul_fp8(A: Fp8, B: Fp8, bias=None, act=0, residual=None, out_dtype=torch.bfloat16, Y=None):
+    """Y = round(act(A B^T + bias) + residual) of quantised A [T, K] (FP8_ROW) and B [M, K]."""
+    native = _native()
+    _here(A.codes, A.scales, B.codes, B.scales, bias, residual, Y)
+    T, M, K = A.rows, B.rows, A.cols
+    if A.layout != FP8_ROW or B.cols != K:
+        raise ValueError("A must be quantised by rows and have the columns of B")
+    _fp8_fits(A)
+    _fp8_fits(B)
+    if Y is None:
+        Y = native.empty(A.codes, _DT[out_dtype], T, M)
+    elif tuple(Y.shape) != (T, M):
+        raise ValueError("Y must be [T, M]")
+    _epilogue_fits(T, M, Y.dtype, bias, residual)
+    need = native.bsp_matmul_fp8_workspace_bytes(T, M, K)
+    ws = _scratch(need, Y.device)
+    st = native.bsp_matmul_fp8(A.codes, A.scales, B.codes, B.scales, B.layout, T, M, K, bias, act, residual, Y, _DT[Y.dtype], ws,
+                               0 if ws is None else need, _stream())
+    _check(st, "bsp_matmul_fp8")
+    return Y
+
+
+def bsp_linear_fp8(X, W: Fp8, bias=None, act=0, residual=None, Y=None, ws=None):
+    """The layer on X [T, N] with quantised weights [M, N]: X brought to 8 bits by rows, and bsp_matmul_fp8."""
+    native = _native()
+    _here(X, W.codes, W.scales, bias, residual, Y, ws)
+    T, N = X.shape
+    if N != W.cols:
+        raise ValueError("X has the wrong number of columns")
+    _fp8_fits(W)
+    if Y is None:
+        Y = native.empty(X, _DT[X.dtype], T, W.rows)
+    elif Y.dtype != X.dtype or tuple(Y.shape) != (T, W.rows):
+        raise ValueError("Y must be a [T, M] tensor of the dtype of X")
+    _epilogue_fits(T, W.rows, X.dtype, bias, residual)
+    if ws is None:
+        ws = native.empty(X, _U8, native.bsp_linear_fp8_workspace_bytes(T, W.rows, N))
+    st = native.bsp_linear_fp8(X, _DT[X.dtype], T, W.rows, N, W.codes, W.scales, W.layout, bias, act, residual, Y, ws,
+                               ws.numel() * ws.element_size(), _stream())
+    _check(st, "bsp_linear_fp8")
+    return Y
+
+
+NORM_LAYER, NORM_RMS = 0, 1
+NORM_POST, NORM_PRE = 1, 2
+
+
+def _norm_fits(like, rows, vectors, gate):
+    T, H = like.shape
+    for x in rows:
+        if x is not None and (x.dtype != like.dtype or x.shape != like.shape):
+            raise ValueError("the [T, H] tensors must share one shape and dtype")
+    for x in vectors:
+        if x is not None and (x.dtype != like.dtype or x.numel() != H):
+            raise ValueError("weights and biases must have H elements of the dtype of the rows")
+    if gate is None:
+        return 0
+    if gate.dtype != like.dtype or gate.dim() not in (1, 2) or gate.shape[-1] != H:
+        raise ValueError("gate must be [gate_rows, H] of the dtype of the rows")
+    return gate.numel() // H
+
+
+def bsp_block_norm(X, F=None, norms=NORM_PRE, kind=NORM_LAYER, eps=1e-12, x_scale=1.0, gate=None, w_post=None, b_post=None, w_pre=None,
+                   b_pre=None, Z=None, H=None, want=("Z", "stats_post", "stats_pre")):
+    """Z = x_scale X + gate * N_post(F), H = N_pre(Z) (norms: NORM_POST, NORM_PRE or both).  Returns (Z, H, stats_post, stats_pre);
+    what is absent or not in `want` (and not passed) is None, without NORM_PRE also H."""
+    native = _native()
+    _here(X, F, gate, w_post, b_post, w_pre, b_pre, Z, H)
+    T, width = X.shape
+    gate_rows = _norm_fits(X, (F, Z, H), (w_post, b_post, w_pre, b_pre), gate)
+    dt = _DT[X.dtype]
+    if Z is None and ("Z" in want or not norms & NORM_PRE):
+        Z = native.empty(X, dt, T, width)
+    if H is None and norms & NORM_PRE:
+        H = native.empty(X, dt, T, width)
+    stats_post = native.empty(X, F32, T, 2) if norms & NORM_POST and "stats_post" in want else None
+    stats_pre = native.empty(X, F32, T, 2) if norms & NORM_PRE and "stats_pre" in want else None
+    st = native.bsp_block_norm(X, F, dt, T, width, norms, kind, eps, x_scale, gate, gate_rows, w_post, b_post, w_pre, b_pre, Z, H,
+                               stats_post, stats_pre, _stream())
+    _check(st, "bsp_block_norm")
+    return Z, H, stats_post, stats_pre
+
+
+def bsp_block_norm_backward(dZ, dH, Z, F=None, norms=NORM_PRE, kind=NORM_LAYER, x_scale=1.0, gate=None, w_post=None, b_post=None,
+                            w_pre=None, b_pre=None, stats_post=None, stats_pre=None, dX=None, dF=None,
+                            want=("dx", "df", "dw_post", "db_post", "dw_pre", "db_pre", "dgate"), ws=None):
+    """Gradients of bsp_block_norm, as a dict of those in `want` that the call has (the others None): dx and df in the dtype of the
+    rows, the sums over the rows in fp32.  dZ, or dH and Z, may be None where the forward pass had no use for them."""
+    native = _native()
+    _here(dZ, dH, Z, F, gate, w_post, b_post, w_pre, b_pre, stats_post, stats_pre, dX, dF, ws)
+    like = dZ if dZ is not None else dH
+    T, H = like.shape
+    gate_rows = _norm_fits(like, (dZ, dH, Z, F, dX, dF), (w_post, b_post, w_pre, b_pre), gate)
+    for stats in (stats_post, stats_pre):
+        if stats is not None and tuple(stats.shape) != (T, 2):
+            raise ValueError("stats must be [T, 2]")
+    dt = _DT[like.dtype]
+    out = {"dx": dX, "df": dF}
+    for name in ("dx", "df"):
+        if out[name] is None and name in want:
+            out[name] = native.empty(like, dt, T, H)
+    for name, place, x in (("dw_post", NORM_POST, w_post), ("db_post", NORM_POST, b_post), ("dw_pre", NORM_PRE, w_pre), ("db_pre", NORM_PRE, b_pre)):
+        out[name] = native.empty(like, F32, H) if x is not None and norms & place and name in want else None
+    out["dgate"] = native.empty(like, F32, gate_rows, H) if gate is not None and "dgate" in want else None
+    need = native.bsp_block_norm_backward_workspace_bytes(T, H, gate_rows)
+    if ws is None and any(out[k] is not None for k in ("dw_post", "db_post", "dw_pre", "db_pre", "dgate")):
+        ws = native.empty(like, _U8, need)
+    st = native.bsp_block_norm_backward(dZ, dH, Z, F, dt, T, H, norms, kind, x_scale, gate, gate_rows, w_post, b_post, w_pre, stats_post,
+                                        stats_pre, out["dx"], out["df"], out["dw_post"], out["db_post"], out["dw_pre"], out["db_pre"],
+                                        out["dgate"], ws, 0 if ws is None else ws.numel() * ws.element_size(), _stream())
+    _check(st, "bsp_block_norm_backward")
+    return out
 
 
 def bsp_compression_rate(M, N, R, kept_cols_total) -> float:

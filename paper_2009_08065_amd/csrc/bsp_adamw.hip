@@ -1,0 +1,413 @@
+// One Adam step with decoupled weight decay over many tensors (bsp_adamw_step): the moments in fp32, or as 8-bit codes with a
+// scale for every 256 elements.
+//
+// A model's step is hundreds of small tensors beside a few large ones, so the tensors' addresses go to the kernel as its
+// arguments (kMaxTensors to a launch: nothing is copied to the device and a captured step needs no memory of its own) and a
+// workgroup finds its tensor by its number.
+//
+// fp32 moments: the arithmetic of bsp_adam_step, one rounding per operation, the decay before the update.
+// 8-bit moments: m and r = sqrt(v) are kept, r because the update divides by it: the codes of e4m3 span 2^18, those of v would
+// span a range of gradients of 2^9 only.  They are rounded up or down at random in proportion to the distance: v changes by a
+// thousandth in a step, a code by a sixteenth, and rounded to the nearest a moment would never move.  The random bits are mixed from the
+// element's place, the step and the seed, so equal calls give equal bits.  A positive r does not become 0: the next step
+// would divide by eps alone.
+#include "bsp_common.h"
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <utility>
+
+namespace bsp {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxTensors = 40;            // 40 entries of 88 bytes: a launch has 4 KB of arguments
+constexpr int kPerThread = 8;              // elements (fp32 moments), 256 apart
+constexpr int kBlock = 256;                // elements of an 8-bit scale: one wavefront, 4 per lane
+constexpr int kBlocksPerWave = 4;
+constexpr int64_t kChunk32 = kThreads * kPerThread, kChunk8 = (kThreads / kWave) * kBlocksPerWave * kBlock;
+
+struct Entry {
+    float *w;
+    const void *g;
+    void *m, *v;
+    float *scales;
+    void *copy;
+    const uint8_t *keep;
+    const float *alpha;
+    int64_t n;
+    uint32_t N, R;
+    float decay;       // lr * weight decay where the host knows lr, else the weight decay
+    uint32_t aligned;  // four elements at a time
+};
+
+struct Table {
+    Entry e[kMaxTensors];
+    uint32_t first[kMaxTensors];  // first workgroup of each tensor
+    int32_t count;
+};
+
+struct Hyper {
+    float lr, beta1, beta2, omb1, omb2, c1, c2, eps, lambda, log1, log2;
+    uint32_t seed, t;
+    const float *lr_t, *grad_scale;
+};
+
+// What a step has in common, and whether it is taken at all.
+struct Step {
+    float lr, c1, c2, gs;
+    uint32_t salt;
+};
+
+__device__ __forceinline__ bool begin_step(const Hyper &h, Step &s) {
+    s.gs = h.grad_scale ? *h.grad_scale : 1.0f;
+    if (!(__builtin_fabsf(s.gs) <= 3.402823466e38f)) return false;
+    uint32_t t = h.t;
+    s.lr = h.lr;
+    s.c1 = h.c1;
+    s.c2 = h.c2;
+    if (h.lr_t) {  // 1 - beta^t without the cancellation of the difference
+        s.lr = h.lr_t[0];
+        const float tf = h.lr_t[1];
+        t = (uint32_t)tf;
+        s.c1 = -expm1f(tf * h.log1);
+        s.c2 = -expm1f(tf * h.log2);
+    }
+    s.salt = h.seed * 0x9E3779B1u + t * 0x6A09E667u;
+    return true;
+}
+
+// The tensor of this workgroup (its index; uniform).
+__device__ __forceinline__ int find_tensor(const Table &tab) {
+    const int lane = threadIdx.x & 63;
+    const bool before = lane < tab.count && tab.first[lane < kMaxTensors ? lane : 0] <= blockIdx.x;
+    return __builtin_popcountll(__ballot(before)) - 1;
+}
+
+// Place of an element in the group arrays [M / R, N]: rows and columns counted from the row that `base` lies in.
+struct Groups {
+    int64_t row0;
+    uint32_t col0, N, R;
+    __device__ __forceinline__ Groups(const Entry &e, int64_t base) : N(e.N), R(e.R) {
+        row0 = e.n <= 0xffffffffll ? (int64_t)((uint32_t)base / N) : base / N;
+        col0 = (uint32_t)(base - row0 * N);
+    }
+    __device__ __forceinline__ int64_t at(uint32_t local) const {
+        const uint32_t c = col0 + local, q = c / N;
+        const int64_t row = row0 + q;
+        const int64_t b = row <= 0xffffffffll ? (int64_t)((uint32_t)row / R) : row / R;
+        return b * N + (c - q * N);
+    }
+};
+
+__device__ __forceinline__ float update(float w, float m, float v, float lr, float c1, float c2, float eps) {
+    const float mh = m / c1;
+    const float vh = v / c2;
+    const float num = lr * mh;
+    const float den = __builtin_sqrtf(vh) + eps;
+    const float q = num / den;
+    return w - q;
+}
+
+template <int CDT>
+__device__ __forceinline__ void store_copy(void *p, int64_t i, float v) {
+    if (p) elem<CDT>::store(p, i, v);
+}
+
+template <int GDT, int CDT>
+__global__ __launch_bounds__(kThreads) void adamw32_kernel(Table tab, Hyper h) {
+    Step s;
+    if (!begin_step(h, s)) return;
+    const int k = find_tensor(tab);
+    const Entry &e = tab.e[k];
+    const int64_t base = (int64_t)(blockIdx.x - tab.first[k]) * kChunk32;
+    float *w = e.w + base, *m = (float *)e.m + base, *v = (float *)e.v + base;
+    const int64_t left = e.n - base;
+    const Groups groups(e, base);
+    const float decay = s.lr * e.decay;
+#pragma unroll 4
+    for (int j = 0; j < kPerThread; ++j) {
+        const uint32_t i = j * kThreads + threadIdx.x;
+        if (i >= left) break;
+        const float w0 = w[i];
+        float g = elem<GDT>::load(e.g, base + i);
+        if (h.grad_scale) g = g * s.gs;
+        int64_t at = 0;
+        if (e.keep || e.alpha) at = groups.at(i);
+        if (e.alpha) g = __builtin_fmaf(h.lambda * e.alpha[at], w0, g);
+        const float t1 = h.beta1 * m[i];
+        const float t2 = h.omb1 * g;
+        const float mn = t1 + t2;
+        const float t3 = h.beta2 * v[i];
+        float t4 = h.omb2 * g;
+        t4 = t4 * g;
+        const float vn = t3 + t4;
+        float wn = w0;
+        if (decay != 0.0f) {
+            const float d = decay * w0;
+            wn = w0 - d;
+        }
+        wn = update(wn, mn, vn, s.lr, s.c1, s.c2, h.eps);
+        if (e.keep && !e.keep[at]) wn = 0.0f;
+        w[i] = wn;
+        m[i] = mn;
+        v[i] = vn;
+        store_copy<CDT>(e.copy, base + i, wn);
+    }
+}
+
+// ---- 8-bit moments ------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t mix(uint32_t x) {
+    x = (x ^ (x >> 16)) * 0xBB67AE85u;
+    x = (x ^ (x >> 15)) * 0x3C6EF373u;
+    return x ^ (x >> 16);
+}
+
+// The largest of 64 lanes' values (all >= 0), in every lane.
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) x = __builtin_fmaxf(x, __shfl_xor(x, d));
+    return x;
+}
+
+// |y| <= 448 to one of the two codes' values next to it, up where the 16 bits (of 2^16) exceed what is missing.  Below 2^-6 the
+// step is that of 2^-6, which the addition of 2^-6 brings about.
+__device__ __forceinline__ float round_random(float y, uint32_t bits16) {
+    const float a = __builtin_fabsf(y);
+    const bool small = a < 0.015625f;
+    const float z = small ? a + 0.015625f : a;
+    const float q = __uint_as_float((__float_as_uint(z) + (bits16 << 4)) & 0xfff00000u);
+    return __builtin_copysignf(small ? q - 0.015625f : q, y);
+}
+
+// four values, each an e4m3 number, as codes
+__device__ __forceinline__ uint32_t codes4(const float (&x)[4]) {
+    int p = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], p, true);
+}
+template <int I>
+__device__ __forceinline__ float value_of(uint32_t codes) {
+    return __builtin_amdgcn_cvt_f32_fp8((int)codes, I);
+}
+
+template <int GDT, int CDT>
+__global__ __launch_bounds__(kThreads) void adamw8_kernel(Table tab, Hyper h) {
+    Step s;
+    if (!begin_step(h, s)) return;
+    const int k = find_tensor(tab);
+    const Entry &e = tab.e[k];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t base = (int64_t)(blockIdx.x - tab.first[k]) * kChunk8 + wave * (kBlocksPerWave * kBlock);
+    const Groups groups(e, base);
+    const int64_t blocks = (e.n + kBlock - 1) / kBlock;
+    const float decay = s.lr * e.decay;
+    uint8_t *m8 = (uint8_t *)e.m, *v8 = (uint8_t *)e.v;
+    for (int b = 0; b < kBlocksPerWave; ++b) {
+        const int64_t i0 = base + b * kBlock + 4 * lane, block = base / kBlock + b;
+        if (block >= blocks) break;  // uniform in a wavefront
+        const int have = e.n - i0 >= 4 ? 4 : (e.n > i0 ? (int)(e.n - i0) : 0);
+        const bool four = e.aligned && have == 4;
+        float w[4] = {0, 0, 0, 0}, g[4] = {0, 0, 0, 0}, m[4], r[4];
+        uint32_t mc = 0, vc = 0;
+        if (four) {
+            const float4 t = *reinterpret_cast<const float4 *>(e.w + i0);
+            w[0] = t.x, w[1] = t.y, w[2] = t.z, w[3] = t.w;
+            mc = *reinterpret_cast<const uint32_t *>(m8 + i0);
+            vc = *reinterpret_cast<const uint32_t *>(v8 + i0);
+            if constexpr (GDT == BSP_F32) {
+                const float4 u = *reinterpret_cast<const float4 *>((const float *)e.g + i0);
+                g[0] = u.x, g[1] = u.y, g[2] = u.z, g[3] = u.w;
+            } else {
+                const uint2 u = *reinterpret_cast<const uint2 *>((const uint16_t *)e.g + i0);
+                const uint16_t c[4] = {(uint16_t)u.x, (uint16_t)(u.x >> 16), (uint16_t)u.y, (uint16_t)(u.y >> 16)};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) g[j] = elem<GDT>::load(&c[j], 0);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j < have) {
+                    w[j] = e.w[i0 + j];
+                    g[j] = elem<GDT>::load(e.g, i0 + j);
+                    mc |= (uint32_t)m8[i0 + j] << (8 * j);
+                    vc |= (uint32_t)v8[i0 + j] << (8 * j);
+                }
+        }
+        const float sm = e.scales[block], sv = e.scales[blocks + block];
+        const float m0[4] = {value_of<0>(mc), value_of<1>(mc), value_of<2>(mc), value_of<3>(mc)};
+        const float r0[4] = {value_of<0>(vc), value_of<1>(vc), value_of<2>(vc), value_of<3>(vc)};
+        float top_m = 0.0f, top_r = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            int64_t at = 0;
+            const bool grouped = (e.keep || e.alpha) && j < have;
+            if (grouped) at = groups.at((uint32_t)(i0 + j - base));
+            float x = g[j];
+            if (h.grad_scale) x = x * s.gs;
+            if (grouped && e.alpha) x = __builtin_fmaf(h.lambda * e.alpha[at], w[j], x);
+            m[j] = h.beta1 * (m0[j] * sm) + h.omb1 * x;
+            const float ro = r0[j] * sv;
+            const float v = h.beta2 * (ro * ro) + h.omb2 * x * x;
+            r[j] = __builtin_sqrtf(v);
+            float wn = w[j];
+            if (decay != 0.0f) {
+                const float d = decay * wn;
+                wn = wn - d;
+            }
+            wn = update(wn, m[j], v, s.lr, s.c1, s.c2, h.eps);
+            if (grouped && e.keep && !e.keep[at]) wn = 0.0f;
+            w[j] = wn;
+            top_m = __builtin_fmaxf(top_m, __builtin_fabsf(m[j]));
+            top_r = __builtin_fmaxf(top_r, r[j]);
+        }
+        top_m = wave_max(top_m);
+        top_r = wave_max(top_r);
+        // (2^-100: below it 448 / largest has no number, and such moments move nothing)
+        const bool has_m = top_m >= 0x1p-100f, has_r = top_r >= 0x1p-100f;
+        const float im = has_m ? 448.0f / top_m : 0.0f, ir = has_r ? 448.0f / top_r : 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t bits = mix((uint32_t)(i0 + j) + s.salt);
+            const float ym = __builtin_fminf(__builtin_fmaxf(m[j] * im, -448.0f), 448.0f), yr = __builtin_fminf(r[j] * ir, 448.0f);
+            m[j] = round_random(ym, bits & 0xffffu);
+            r[j] = yr > 0.0f ? __builtin_fmaxf(round_random(yr, bits >> 16), 0x1p-9f) : 0.0f;
+        }
+        const uint32_t mn = codes4(m), vn = codes4(r);
+        if (lane == 0) {
+            e.scales[block] = has_m ? top_m * (1.0f / 448.0f) : 0.0f;
+            e.scales[blocks + block] = has_r ? top_r * (1.0f / 448.0f) : 0.0f;
+        }
+        if (four) {
+            *reinterpret_cast<float4 *>(e.w + i0) = make_float4(w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<uint32_t *>(m8 + i0) = mn;
+            *reinterpret_cast<uint32_t *>(v8 + i0) = vn;
+            if (e.copy)
+                *reinterpret_cast<uint2 *>((uint16_t *)e.copy + i0) = make_uint2(elem<CDT>::bits(w[0]) | (elem<CDT>::bits(w[1]) << 16),
+                                                                                 elem<CDT>::bits(w[2]) | (elem<CDT>::bits(w[3]) << 16));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j < have) {
+                    e.w[i0 + j] = w[j];
+                    m8[i0 + j] = (uint8_t)(mn >> (8 * j));
+                    v8[i0 + j] = (uint8_t)(vn >> (8 * j));
+                    store_copy<CDT>(e.copy, i0 + j, w[j]);
+                }
+        }
+    }
+}
+
+template <int GDT>
+void launch(const Table &tab, const Hyper &h, unsigned wgs, int bits, int cdt, hipStream_t s) {
+    if (bits == 32) {
+        if (cdt == BSP_F16) adamw32_kernel<GDT, BSP_F16><<<wgs, kThreads, 0, s>>>(tab, h);
+        else adamw32_kernel<GDT, BSP_BF16><<<wgs, kThreads, 0, s>>>(tab, h);
+    } else {
+        if (cdt == BSP_F16) adamw8_kernel<GDT, BSP_F16><<<wgs, kThreads, 0, s>>>(tab, h);
+        else adamw8_kernel<GDT, BSP_BF16><<<wgs, kThreads, 0, s>>>(tab, h);
+    }
+}
+
+// Whether two tensors' weights share memory (a tied tensor that is listed twice would be updated by two workgroups at once).
+// 0 no, 1 yes, -1 no memory to find out.  In ascending order, as models allocate them, one look is enough.
+int overlapping(const bsp_adamw_tensor *x, int64_t count) {
+    const float *end = nullptr;
+    bool ascending = true;
+    for (int64_t i = 0; i < count && ascending; ++i) {
+        if (x[i].M == 0 || x[i].N == 0) continue;
+        ascending = x[i].w >= end;
+        end = x[i].w + x[i].M * x[i].N;
+    }
+    if (ascending) return 0;
+    using Range = std::pair<const float *, const float *>;
+    Range *r = new (std::nothrow) Range[(size_t)count];
+    if (!r) return -1;
+    int64_t n = 0;
+    for (int64_t i = 0; i < count; ++i)
+        if (x[i].M && x[i].N) r[n++] = {x[i].w, x[i].w + x[i].M * x[i].N};
+    std::sort(r, r + n);
+    int found = 0;
+    for (int64_t i = 1; i < n; ++i) found |= r[i].first < r[i - 1].second;
+    delete[] r;
+    return found;
+}
+
+}  // namespace
+}  // namespace bsp
+
+using namespace bsp;
+
+extern "C" int bsp_adamw_step(const bsp_adamw_tensor *tensors, int64_t count, int gdt, int cdt, int state_bits, float lambda, float lr,
+                              float beta1, float beta2, float eps, int64_t t, uint32_t seed, const float *lr_t,
+                              const float *grad_scale, void *stream) {
+    if (count < 0 || (state_bits != 32 && state_bits != 8)) return BSP_ERR_SHAPE;
+    if (count && !tensors) return BSP_ERR_NULL;
+    if (!valid_dtype(gdt) || (cdt != BSP_BF16 && cdt != BSP_F16)) return BSP_ERR_DTYPE;
+    if (!lr_t && t < 1) return BSP_ERR_SHAPE;
+    const int64_t chunk = state_bits == 32 ? kChunk32 : kChunk8;
+    for (int64_t i = 0; i < count; ++i) {  // all of them before the first launch
+        const bsp_adamw_tensor &x = tensors[i];
+        if (x.M < 0 || x.N < 0 || x.N > 0x7fffffff || (x.M && x.N > 0x7fffffffffffll / x.M)) return BSP_ERR_SHAPE;
+        if (x.M == 0 || x.N == 0) continue;
+        if (!x.w || !x.g || !x.m || !x.v || (state_bits == 8 && !x.scales)) return BSP_ERR_NULL;
+        if ((x.keep || x.alpha) && (x.R <= 0 || x.M % x.R != 0)) return BSP_ERR_SHAPE;
+        if ((x.M * x.N + chunk - 1) / chunk >= ((int64_t)1 << 31)) return BSP_ERR_SHAPE;
+        if (!aligned(x.w, 4) || !aligned(x.g, dtype_size(gdt)) || (state_bits == 32 && (!aligned(x.m, 4) || !aligned(x.v, 4))) ||
+            !aligned(x.scales, 4) || !aligned(x.copy, 2) || !aligned(x.alpha, 4))
+            return BSP_ERR_SHAPE;
+    }
+    if (const int shared = overlapping(tensors, count)) return shared > 0 ? BSP_ERR_SHAPE : BSP_ERR_CAPACITY;
+    Hyper h;
+    h.lr = lr;
+    h.beta1 = beta1;
+    h.beta2 = beta2;
+    h.omb1 = 1.0f - beta1;
+    h.omb2 = 1.0f - beta2;
+    h.c1 = (float)(1.0 - std::pow((double)beta1, (double)t));
+    h.c2 = (float)(1.0 - std::pow((double)beta2, (double)t));
+    h.eps = eps;
+    h.lambda = lambda;
+    h.log1 = (float)std::log((double)beta1);
+    h.log2 = (float)std::log((double)beta2);
+    h.seed = seed;
+    h.t = (uint32_t)t;
+    h.lr_t = lr_t;
+    h.grad_scale = grad_scale;
+    hipStream_t s = (hipStream_t)stream;
+    Table tab;
+    int64_t wgs = 0;
+    tab.count = 0;
+    auto flush = [&]() -> int {
+        if (!tab.count) return BSP_OK;
+        BSP_DISPATCH_DTYPE(gdt, GDT, { launch<GDT>(tab, h, (unsigned)wgs, state_bits, cdt, s); });
+        tab.count = 0;
+        wgs = 0;
+        return check_launch();
+    };
+    for (int64_t i = 0; i < count; ++i) {
+        const bsp_adamw_tensor &x = tensors[i];
+        const int64_t n = x.M * x.N;
+        if (n == 0) continue;
+        const int64_t need = (n + chunk - 1) / chunk;
+        if (tab.count == kMaxTensors || wgs + need >= ((int64_t)1 << 31))
+            if (int st = flush()) return st;
+        Entry &e = tab.e[tab.count];
+        e.w = x.w;
+        e.g = x.g;
+        e.m = x.m;
+        e.v = x.v;
+        e.scales = x.scales;
+        e.copy = x.copy;
+        e.keep = x.keep;
+        e.alpha = x.alpha;
+        e.n = n;
+        e.N = (uint32_t)x.N;
+        e.R = (uint32_t)(x.R > 0 ? x.R : 1);
+        e.decay = x.weight_decay;
+        e.aligned = aligned(x.w, 16) && aligned(x.g, 4 * dtype_size(gdt)) && aligned(x.m, 4) && aligned(x.v, 4) && aligned(x.copy, 8);
+        tab.first[tab.count++] = (uint32_t)wgs;
+        wgs += need;
+    }
+    return flush();
+}

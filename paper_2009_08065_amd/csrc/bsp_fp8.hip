@@ -1,0 +1,161 @@
+// Matrices in 8-bit floating point (e4m3) with a power of two for every 128 columns of a row, or for every 128 x 128 block
+// (bsp_fp8_quant).
+//
+// The scale of a segment is the least power of two that brings its largest value to 448, e4m3's largest, or below.  It is held as
+// a biased exponent in one byte, which the matrix instruction of the product takes as it is: no multiplication is spent on
+// scales there, and a code times its scale has no rounding of its own.  Against a scale of largest / 448 it leaves at most one of the
+// type's 18 binades unused.
+//
+// Bound by memory: a workgroup reads a 128 x 128 tile once, 8 x 8 values per thread, and has from it the row segments, the column
+// segments (the rows of the transposed matrix) or the block, and the codes of either orientation; the transposed ones go through LDS.
+#include "bsp_common.h"
+#include "bsp_fp8_device.h"
+
+namespace bsp {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPitch = 128 + 8;  // bytes of a column's codes in LDS: 8-byte writes of 16 threads fall into different banks
+
+struct Quant {
+    const void *X;
+    uint8_t *Q, *S, *Qt, *St;
+    int64_t rows, cols, tiles_c, pitch, pitch_t;  // pitches of Q and Qt: columns and rows, padded to 128
+    int32_t vec;
+};
+
+template <int DT, bool BLOCK, bool TRANSPOSED>
+__global__ __launch_bounds__(kThreads) void quant_kernel(Quant a) {
+    __shared__ float top[TRANSPOSED ? 4 * 128 : 4];
+    __shared__ __align__(16) uint8_t turned[TRANSPOSED ? 128 * kPitch : 16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t tr = blockIdx.x / a.tiles_c, tc = blockIdx.x - tr * a.tiles_c;
+    const int r0 = 8 * (tid >> 4), c0 = 8 * (tid & 15);
+    const int64_t row0 = 128 * tr + r0, col0 = 128 * tc + c0;
+    const int rows = a.rows - row0 > 8 ? 8 : (int)(a.rows - row0), cols = a.cols - col0 > 8 ? 8 : (int)(a.cols - col0);  // (may be negative)
+
+    float v[8][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int64_t at = (row0 + i) * a.cols + col0;
+        if (i < rows && cols == 8 && a.vec) {
+            if constexpr (DT == BSP_F32) {
+                const float4 p = *reinterpret_cast<const float4 *>((const float *)a.X + at);
+                const float4 q = *reinterpret_cast<const float4 *>((const float *)a.X + at + 4);
+                v[i][0] = p.x, v[i][1] = p.y, v[i][2] = p.z, v[i][3] = p.w, v[i][4] = q.x, v[i][5] = q.y, v[i][6] = q.z, v[i][7] = q.w;
+            } else {
+                unpack8<DT>(*reinterpret_cast<const uint4 *>((const uint16_t *)a.X + at), v[i]);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] = i < rows && j < cols ? elem<DT>::load(a.X, at + j) : 0.0f;
+        }
+    }
+
+    uint32_t e_row[8], e_col[8];  // biased exponents of the rows' and the columns' scales
+    if constexpr (BLOCK) {
+        float m = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m = __builtin_fmaxf(m, magnitude(v[i][j]));
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d));
+        if (lane == 0) top[wave] = m;
+        __syncthreads();
+        m = __builtin_fmaxf(__builtin_fmaxf(top[0], top[1]), __builtin_fmaxf(top[2], top[3]));
+        const uint32_t e = scale_exponent(m);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e_row[i] = e_col[i] = e;
+        if (tid == 0) {
+            if (a.Q) a.S[tr * a.tiles_c + tc] = (uint8_t)e;
+            if (TRANSPOSED) a.St[tc * (a.pitch_t / 128) + tr] = (uint8_t)e;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float m = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m = __builtin_fmaxf(m, magnitude(v[i][j]));
+#pragma unroll
+            for (int d = 1; d < 16; d <<= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d));
+            e_row[i] = scale_exponent(m);
+            if (a.Q && (tid & 15) == 0 && i < rows) a.S[(row0 + i) * a.tiles_c + tc] = (uint8_t)e_row[i];
+        }
+        if constexpr (TRANSPOSED) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float m = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) m = __builtin_fmaxf(m, magnitude(v[i][j]));
+                m = __builtin_fmaxf(m, __shfl_xor(m, 16));
+                m = __builtin_fmaxf(m, __shfl_xor(m, 32));
+                if (lane < 16) top[wave * 128 + c0 + j] = m;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int c = c0 + j;
+                e_col[j] = scale_exponent(__builtin_fmaxf(__builtin_fmaxf(top[c], top[128 + c]), __builtin_fmaxf(top[256 + c], top[384 + c])));
+                if (tid < 16 && j < cols) a.St[(col0 + j) * (a.pitch_t / 128) + tr] = (uint8_t)e_col[j];
+            }
+        }
+    }
+
+    if (a.Q) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (i >= rows) break;
+            const float s = inverse_scale(e_row[i]);
+            float y[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = s * v[i][j];
+            *reinterpret_cast<uint2 *>(a.Q + (row0 + i) * a.pitch + col0) = make_uint2(codes4(y), codes4(y + 4));
+        }
+    }
+    if constexpr (TRANSPOSED) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float s = inverse_scale(e_col[j]);
+            float y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = s * v[i][j];
+            *reinterpret_cast<uint2 *>(turned + (c0 + j) * kPitch + r0) = make_uint2(codes4(y), codes4(y + 4));
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int c = (tid >> 4) + 16 * i;
+            if (128 * tc + c < a.cols)
+                *reinterpret_cast<uint2 *>(a.Qt + (128 * tc + c) * a.pitch_t + 128 * tr + 8 * (tid & 15)) =
+                    *reinterpret_cast<const uint2 *>(turned + c * kPitch + 8 * (tid & 15));
+        }
+    }
+}
+
+template <int DT>
+void launch(const Quant &a, unsigned grid, bool block, bool transposed, hipStream_t s) {
+    if (block && transposed) quant_kernel<DT, true, true><<<grid, kThreads, 0, s>>>(a);
+    else if (block) quant_kernel<DT, true, false><<<grid, kThreads, 0, s>>>(a);
+    else if (transposed) quant_kernel<DT, false, true><<<grid, kThreads, 0, s>>>(a);
+    else quant_kernel<DT, false, false><<<grid, kThreads, 0, s>>>(a);
+}
+
+}  // namespace
+}  // namespace bsp
+
+using namespace bsp;
+
+extern "C" int bsp_fp8_quant(const void *X, int xdt, int64_t rows, int64_t cols, int layout, void *Q, uint8_t *S, void *Qt, uint8_t *St,
+                             void *stream) {
+    if (!valid_dtype(xdt) || (layout != BSP_FP8_ROW && layout != BSP_FP8_BLOCK)) return BSP_ERR_DTYPE;
+    if (rows < 0 || cols <= 0 || cols >= ((int64_t)1 << 31) || rows >= ((int64_t)1 << 31)) return BSP_ERR_SHAPE;
+    if (rows == 0 || (!Q && !Qt)) return BSP_OK;
+    if (!X || (Q && !S) || (Qt && !St)) return BSP_ERR_NULL;
+    if (!aligned(X, dtype_size(xdt)) || !aligned(Q, 16) || !aligned(Qt, 16)) return BSP_ERR_SHAPE;
+    const int64_t tiles_r = (rows + 127) / 128, tiles_c = (cols + 127) / 128;
+    if (tiles_r * tiles_c >= ((int64_t)1 << 31)) return BSP_ERR_SHAPE;
+    const Quant a = {X, (uint8_t *)Q, S, (uint8_t *)Qt, St, rows, cols, tiles_c, 128 * tiles_c, 128 * tiles_r, aligned(X, 16) && cols % 8 == 0};
+    BSP_DISPATCH_DTYPE(xdt, DT, { launch<DT>(a, (unsigned)(tiles_r * tiles_c), layout == BSP_FP8_BLOCK, Qt != nullptr, (hipStream_t)stream); });
+    return check_launch();
+}

@@ -1,0 +1,373 @@
+// Products of 8-bit matrices: Y = act(A B^T + bias) + residual (bsp_matmul_fp8), and the layer on 16- or 32-bit inputs
+// (bsp_linear_fp8).
+//
+// Both operands have 128-column segments of one power of two each (bsp_fp8.hip), so a step of 128 columns is two
+// v_mfma_scale_f32_32x32x64 per 32 x 32 piece, which take the codes and, per lane, the biased exponents of the lane's row: the sums come
+// out scaled, in fp32, without a vector instruction.
+//
+// That instruction (like the unscaled ones on 8-bit codes) brings the products of a lane to the largest one's exponent before it adds
+// them and drops what is 14 binades below: 1.3e-5 of the result (2-norm, N(0, 1) operands) whatever the length, far below the rounding to 16
+// bits and below that of the operands, but not fp32.  So results in fp32 take the same codes through v_mfma_f32_32x32x16_bf16: a code times its
+// scale is a bfloat16, the conversion applies it, and 6e-9 of the result is what is lost, at half the rate.
+//
+// The roles: B's rows (output columns) are the instruction's rows, A's rows (tokens) its columns, so that a lane ends with groups of four
+// consecutive outputs of one token.
+//
+// A workgroup owns 32 FB WB tokens x 32 FA WA outputs; both tiles go straight from memory to LDS, 128 bytes of a row at a time, two steps in
+// turn.  A row's 16-byte pieces are rotated by half its number, which the loads bring about by what each lane asks for, so that
+// the operand reads of 16 lanes meet all banks.
+#include "bsp_common.h"
+#include "bsp_fp8_device.h"
+#include "bsp_mfma_device.h"
+#include "bsp_tile_device.h"
+
+namespace bsp {
+namespace {
+
+struct Product {
+    const uint8_t *A, *SA, *B, *SB;
+    const void *bias, *residual;
+    void *Y;
+    float *partial;  // [splits][T][M] where the columns are split, else null
+    int64_t T, M;
+    int32_t steps, pitch, split_steps;  // steps of 128 columns; bytes of a row; steps of a split
+    int32_t block, act;                 // B has a scale per 128 rows
+};
+
+__device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
+
+// Four scales at index i of an array of `total`, read as one word where it is inside; the bytes past the end are of no interest.
+__device__ __forceinline__ uint32_t scales4(const uint8_t *s, int64_t i, int64_t total) {
+    uint32_t v = 0;
+    if (i + 4 <= total) {
+        __builtin_memcpy(&v, s + i, 4);
+    } else {
+        for (int k = 0; k < 3; ++k)
+            if (i + k < total) v |= (uint32_t)s[i + k] << (8 * k);
+    }
+    return v;
+}
+
+__device__ __forceinline__ f32x16 mfma_scaled(i32x8 a, i32x8 b, f32x16 c, uint32_t sa, uint32_t sb) {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, (int)sa, 0, (int)sb);
+}
+
+// Eight codes times their scale as bfloat16 (exact).
+__device__ __forceinline__ uint4 widen8(uint32_t lo, uint32_t hi, uint32_t scale) {
+    const float f = __uint_as_float(scale << 23);  // (the conversion takes the exponent: 0 is 2^-127)
+    return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, f, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, f, true)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, f, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, f, true)));
+}
+
+// The tile's place: workgroup ids go round the 8 XCDs; each XCD owns whole groups of kGroup token tiles and walks their output ranges.
+constexpr uint32_t kGroup = 4;
+
+template <int DT, int FA, int FB, int WA, int WB>
+__global__ __launch_bounds__(64 * WA * WB) void fp8_tile_kernel(Product p) {
+    constexpr int kWaves = WA * WB, kThreads = 64 * kWaves;
+    constexpr int TA = 32 * FA * WA, TB = 32 * FB * WB;  // outputs, tokens
+    constexpr int kStage = (TA + TB) * 128, kLoads = (TA + TB) / 8 / kWaves;
+    constexpr int kPitch = TA + 4;  // floats of a token's row in the output pass
+    static_assert((TA + TB) / 8 % kWaves == 0);
+    extern __shared__ __align__(16) uint8_t smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, half = lane >> 5;
+    const int wa = wave % WA, wb = wave / WA;
+
+    const uint32_t ranges = (uint32_t)((p.M + TA - 1) / TA), tiles = (uint32_t)((p.T + TB - 1) / TB);
+    const uint32_t per_xcd = (tiles + 7) / 8, place = blockIdx.x >> 3;
+    const uint32_t group = place / (kGroup * ranges), in_group = place - group * kGroup * ranges;
+    const uint32_t height = per_xcd - group * kGroup < kGroup ? per_xcd - group * kGroup : kGroup;
+    const uint32_t tile = (group * kGroup + in_group % height) * 8 + (blockIdx.x & 7);
+    const int64_t t0 = (int64_t)tile * TB, m0 = (int64_t)(in_group / height) * TA;
+    if (t0 >= p.T) return;  // uniform: before any barrier
+    const int first = blockIdx.y * p.split_steps, last = first + p.split_steps < p.steps ? first + p.split_steps : p.steps;
+
+    // the loads of this wavefront: 8 rows each, first B's, then A's; a row past the end reads the last one
+    const uint8_t *base[2] = {p.B + m0 * p.pitch, p.A + t0 * p.pitch};
+    uint32_t at[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const int r8 = wave * kLoads + i, op = 8 * r8 >= TA, r = 8 * r8 + (lane >> 3) - (op ? TA : 0);
+        const int64_t left = op ? p.T - t0 : p.M - m0;
+        const uint32_t row = r < left ? r : (uint32_t)(left - 1);
+        at[i] = row * (uint32_t)p.pitch + ((((uint32_t)lane & 7) ^ ((r >> 1) & 7)) << 4);
+    }
+    auto load = [&](int step, int slot) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int r8 = wave * kLoads + i, op = 8 * r8 >= TA;
+            load_to_lds(slot * kStage + r8 * 1024, base[op] + (int64_t)step * 128, at[i]);
+        }
+    };
+    // scales: of the lane's row of each piece, four steps to a word
+    const int64_t rows_b = p.block ? (p.M + 127) / 128 : p.M, total_a = p.T * p.steps, total_b = rows_b * p.steps;
+    int64_t s_at[FA + FB];
+#pragma unroll
+    for (int f = 0; f < FA; ++f) {
+        int64_t r = m0 + wa * 32 * FA + 32 * f + l32;
+        if (r >= p.M) r = p.M - 1;
+        s_at[f] = (p.block ? r / 128 : r) * p.steps;
+    }
+#pragma unroll
+    for (int f = 0; f < FB; ++f) {
+        int64_t r = t0 + wb * 32 * FB + 32 * f + l32;
+        if (r >= p.T) r = p.T - 1;
+        s_at[FA + f] = r * p.steps;
+    }
+    uint32_t sc[FA + FB], next[FA + FB];
+    auto ask_scales = [&](int step) {
+#pragma unroll
+        for (int f = 0; f < FA + FB; ++f)
+            next[f] = step < last ? scales4(f < FA ? p.SB : p.SA, s_at[f] + step, f < FA ? total_b : total_a) : 0u;
+    };
+
+    f32x16 acc[FA][FB];
+#pragma unroll
+    for (int i = 0; i < FA; ++i)
+#pragma unroll
+        for (int j = 0; j < FB; ++j)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.0f;
+
+    const uint32_t cell = (uint32_t)l32 * 128 + ((((uint32_t)half * 2) ^ ((l32 >> 1) & 7)) << 4);
+    const uint32_t cell_a = cell + (uint32_t)(wa * FA) * 4096, cell_b = cell + TA * 128 + (uint32_t)(wb * FB) * 4096;
+    auto operand = [&](uint32_t c, int slot, int f, int sub) {
+        const uint8_t *q = smem + slot * kStage + f * 4096;
+        const uint4 lo = *reinterpret_cast<const uint4 *>(q + (c ^ (sub << 6))), hi = *reinterpret_cast<const uint4 *>(q + (c ^ (sub << 6) ^ 16));
+        return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+    };
+
+    ask_scales(first);
+    load(first, 0);
+    for (int s = first; s < last; ++s) {
+        const int slot = (s - first) & 1;
+        wait_loads<0>();
+        barrier();  // this step is in LDS, and nobody reads the other slot any more
+        if (((s - first) & 3) == 0) {
+#pragma unroll
+            for (int f = 0; f < FA + FB; ++f) {
+                sc[f] = next[f];
+                asm volatile("" : "+v"(sc[f]));  // (waited for here, before the next loads are on their way)
+            }
+            ask_scales(s + 4);
+        } else {
+#pragma unroll
+            for (int f = 0; f < FA + FB; ++f) sc[f] >>= 8;
+        }
+        if (s + 1 < last) load(s + 1, slot ^ 1);
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub) {
+            i32x8 a[FA], b[FB];
+#pragma unroll
+            for (int i = 0; i < FA; ++i) a[i] = operand(cell_a, slot, i, sub);
+#pragma unroll
+            for (int j = 0; j < FB; ++j) b[j] = operand(cell_b, slot, j, sub);
+            if constexpr (DT == BSP_F32) {
+                static_for<0, 4>([&](auto kk) {
+                    constexpr int k = 2 * decltype(kk)::value;
+                    uint4 wa8[FA], wb8[FB];
+#pragma unroll
+                    for (int i = 0; i < FA; ++i) wa8[i] = widen8((uint32_t)a[i][k], (uint32_t)a[i][k + 1], sc[i] & 0xffu);
+#pragma unroll
+                    for (int j = 0; j < FB; ++j) wb8[j] = widen8((uint32_t)b[j][k], (uint32_t)b[j][k + 1], sc[FA + j] & 0xffu);
+#pragma unroll
+                    for (int i = 0; i < FA; ++i)
+#pragma unroll
+                        for (int j = 0; j < FB; ++j) acc[i][j] = mfma32<BSP_BF16>(wa8[i], wb8[j], acc[i][j]);
+                });
+            } else {
+#pragma unroll
+                for (int i = 0; i < FA; ++i)
+#pragma unroll
+                    for (int j = 0; j < FB; ++j) acc[i][j] = mfma_scaled(a[i], b[j], acc[i][j], sc[i], sc[FA + j]);
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+
+    // A pass of 32 WB tokens: sums to LDS, then whole rows leave with bias, activation and residual
+    float *out = reinterpret_cast<float *>(smem);
+    const bool vec = (p.M & 7) == 0;
+    constexpr int kPiece = TA / 8;  // threads of a row
+    const int c = (tid % kPiece) * 8;
+    const int64_t m = m0 + c;
+    const int cols = p.M - m > 8 ? 8 : (int)(p.M - m);
+    float bias[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) bias[k] = p.bias && !p.partial && k < cols ? elem<DT>::load(p.bias, m + k) : 0.0f;
+#pragma unroll
+    for (int j = 0; j < FB; ++j) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < FA; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<f32x4 *>(out + (wb * 32 + l32) * kPitch + (wa * FA + i) * 32 + 8 * q + 4 * half) =
+                    f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        __syncthreads();
+        for (int r = tid / kPiece; r < 32 * WB; r += kThreads / kPiece) {
+            const int64_t t = t0 + (r >> 5) * 32 * FB + 32 * j + (r & 31);
+            if (t >= p.T || cols <= 0) continue;
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const f32x4 x = *reinterpret_cast<const f32x4 *>(out + r * kPitch + c + 4 * k);
+#pragma unroll
+                for (int n = 0; n < 4; ++n) v[4 * k + n] = x[n];
+            }
+            if (p.partial) {
+                float *y = p.partial + ((int64_t)blockIdx.y * p.T + t) * p.M + m;
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < cols) y[k] = v[k];
+                continue;
+            }
+            const int64_t y = t * p.M + m;
+            finish8<DT>(v, bias, p.act, p.residual, p.Y, y, vec, cols);
+        }
+    }
+}
+
+// The splits' sums, ascending, then bias, activation and residual.
+template <int DT>
+__global__ __launch_bounds__(256) void fp8_join_kernel(Product p, int splits) {
+    const int64_t per_row = (p.M + 7) / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t t = i / per_row, m = (i - t * per_row) * 8;
+    if (t >= p.T) return;
+    const int cols = p.M - m > 8 ? 8 : (int)(p.M - m);
+    float v[8], bias[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        v[k] = 0.0f;
+        bias[k] = p.bias && k < cols ? elem<DT>::load(p.bias, m + k) : 0.0f;
+    }
+    for (int s = 0; s < splits; ++s) {
+        const float *x = p.partial + ((int64_t)s * p.T + t) * p.M + m;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k < cols) v[k] += x[k];
+    }
+    finish8<DT>(v, bias, p.act, p.residual, p.Y, t * p.M + m, (p.M & 7) == 0, cols);
+}
+
+// 1 where the product is not split.
+struct Shape {
+    int tile;    // 256, 128 or 64
+    int splits, split_steps;
+};
+
+Shape choose(int64_t T, int64_t M, int64_t steps) {
+    Shape s = {256, 1, (int)steps};
+    auto count = [&](int64_t t) { return ((T + t - 1) / t) * ((M + t - 1) / t); };
+    if (count(256) < 192) s.tile = 128;
+    if (s.tile == 128 && count(128) < 192) s.tile = 64;
+    const int64_t n = count(s.tile);
+    if (n < 128 && steps >= 8) {
+        int64_t k = 256 / n;
+        if (k > steps / 4) k = steps / 4;
+        if (k > 1) {
+            s.split_steps = (int)((steps + k - 1) / k);
+            s.splits = (int)((steps + s.split_steps - 1) / s.split_steps);
+        }
+    }
+    return s;
+}
+
+template <int DT, int FA, int FB, int WA, int WB>
+int launch_tile(const Product &p, int splits, hipStream_t s) {
+    constexpr int TA = 32 * FA * WA, TB = 32 * FB * WB;
+    constexpr size_t stages = 2 * (size_t)(TA + TB) * 128, out = (size_t)32 * WB * (TA + 4) * 4, lds = stages > out ? stages : out;
+    auto k = fp8_tile_kernel<DT, FA, FB, WA, WB>;
+    if (lds > 65536) {  // (asking again is harmless)
+        hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) {
+            set_last_hip_error((int)e);
+            return BSP_ERR_HIP;
+        }
+    }
+    const int64_t wgs = ((p.T + TB - 1) / TB + 7) / 8 * 8 * ((p.M + TA - 1) / TA);
+    if (wgs >= ((int64_t)1 << 31)) return BSP_ERR_SHAPE;
+    k<<<dim3((unsigned)wgs, (unsigned)splits), 64 * WA * WB, lds, s>>>(p);
+    return check_launch();
+}
+
+template <int DT>
+int launch_product(const Product &p, const Shape &c, hipStream_t s) {
+    int st;
+    if (c.tile == 256) st = launch_tile<DT, 2, 4, 4, 2>(p, c.splits, s);
+    else if (c.tile == 128) st = launch_tile<DT, 2, 2, 2, 2>(p, c.splits, s);
+    else st = launch_tile<DT, 1, 1, 2, 2>(p, c.splits, s);
+    if (st || c.splits == 1) return st;
+    const int64_t n = p.T * ((p.M + 7) / 8);
+    fp8_join_kernel<DT><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(p, c.splits);
+    return check_launch();
+}
+
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+int64_t steps_of(int64_t K) { return (K + 127) / 128; }
+
+size_t split_bytes(int64_t T, int64_t M, int64_t K) {
+    const Shape c = choose(T, M, steps_of(K));
+    return c.splits > 1 ? (size_t)c.splits * (size_t)T * (size_t)M * 4 : 0;
+}
+
+int check_sizes(int64_t T, int64_t M, int64_t K, int layout, int ydt, int act) {
+    if (!valid_dtype(ydt) || (layout != BSP_FP8_ROW && layout != BSP_FP8_BLOCK) || (act != BSP_ACT_NONE && act != BSP_ACT_GELU)) return BSP_ERR_DTYPE;
+    if (T < 0 || M <= 0 || K <= 0 || T >= ((int64_t)1 << 31) || M >= ((int64_t)1 << 31) || K > ((int64_t)1 << 23)) return BSP_ERR_SHAPE;
+    return BSP_OK;
+}
+
+int product(const void *A, const uint8_t *SA, const void *B, const uint8_t *SB, int layout, int64_t T, int64_t M, int64_t K, const void *bias,
+            int act, const void *residual, void *Y, int ydt, void *ws, size_t ws_bytes, hipStream_t s) {
+    Shape c = choose(T, M, steps_of(K));
+    if (c.splits > 1 && ws_bytes < (size_t)c.splits * (size_t)T * (size_t)M * 4) c.splits = 1, c.split_steps = (int)steps_of(K);
+    const Product p = {(const uint8_t *)A, SA, (const uint8_t *)B, SB, bias, residual, Y, c.splits > 1 ? (float *)ws : nullptr, T, M,
+                       (int32_t)steps_of(K), (int32_t)(128 * steps_of(K)), c.split_steps, layout == BSP_FP8_BLOCK, act};
+    switch (ydt) {
+        case BSP_F32: return launch_product<BSP_F32>(p, c, s);
+        case BSP_BF16: return launch_product<BSP_BF16>(p, c, s);
+        default: return launch_product<BSP_F16>(p, c, s);
+    }
+}
+
+}  // namespace
+}  // namespace bsp
+
+using namespace bsp;
+
+extern "C" size_t bsp_matmul_fp8_workspace_bytes(int64_t T, int64_t M, int64_t K) {
+    return T > 0 && !check_sizes(T, M, K, BSP_FP8_ROW, BSP_F32, BSP_ACT_NONE) ? split_bytes(T, M, K) : 0;
+}
+
+extern "C" int bsp_matmul_fp8(const void *A, const uint8_t *SA, const void *B, const uint8_t *SB, int b_layout, int64_t T, int64_t M, int64_t K,
+                              const void *bias, int act, const void *residual, void *Y, int ydt, void *ws, size_t ws_bytes, void *stream) {
+    if (int st = check_sizes(T, M, K, b_layout, ydt, act)) return st;
+    if (T == 0) return BSP_OK;
+    if (!A || !SA || !B || !SB || !Y) return BSP_ERR_NULL;
+    const size_t size = dtype_size(ydt);
+    if (!aligned(A, 16) || !aligned(B, 16) || !aligned(Y, size) || !aligned(bias, size) || !aligned(residual, size) || !aligned(ws, 256)) return BSP_ERR_SHAPE;
+    if (!ws) ws_bytes = 0;
+    if (ws_bytes && ws_bytes < split_bytes(T, M, K)) return BSP_ERR_CAPACITY;
+    return product(A, SA, B, SB, b_layout, T, M, K, bias, act, residual, Y, ydt, ws, ws_bytes, (hipStream_t)stream);
+}
+
+extern "C" size_t bsp_linear_fp8_workspace_bytes(int64_t T, int64_t M, int64_t N) {
+    if (T <= 0 || check_sizes(T, M, N, BSP_FP8_ROW, BSP_F32, BSP_ACT_NONE)) return 0;
+    return up256((size_t)T * 128 * steps_of(N)) + up256((size_t)T * steps_of(N)) + split_bytes(T, M, N);
+}
+
+extern "C" int bsp_linear_fp8(const void *X, int xdt, int64_t T, int64_t M, int64_t N, const void *W, const uint8_t *SW, int w_layout,
+                              const void *bias, int act, const void *residual, void *Y, void *ws, size_t ws_bytes, void *stream) {
+    if (int st = check_sizes(T, M, N, w_layout, xdt, act)) return st;
+    if (T == 0) return BSP_OK;
+    if (!X || !W || !SW || !Y || !ws) return BSP_ERR_NULL;
+    const size_t size = dtype_size(xdt);
+    if (!aligned(X, size) || !aligned(W, 16) || !aligned(Y, size) || !aligned(bias, size) || !aligned(residual, size) || !aligned(ws, 256)) return BSP_ERR_SHAPE;
+    if (ws_bytes < bsp_linear_fp8_workspace_bytes(T, M, N)) return BSP_ERR_CAPACITY;
+    uint8_t *codes = (uint8_t *)ws, *scales = codes + up256((size_t)T * 128 * steps_of(N)), *rest = scales + up256((size_t)T * steps_of(N));
+    if (int st = bsp_fp8_quant(X, xdt, T, N, BSP_FP8_ROW, codes, scales, nullptr, nullptr, stream)) return st;
+    return product(codes, scales, W, SW, w_layout, T, M, N, bias, act, residual, Y, xdt, rest, split_bytes(T, M, N), (hipStream_t)stream);
+}

@@ -21,6 +21,7 @@
 #include <tuple>
 #include <type_traits>
 #include <utility>
+#include <vector>
 
 #include "bsp.h"
 
@@ -219,20 +220,20 @@ PyObject *empty_beside_other(PyObject *like, const char *type, const int64_t *si
     return result;
 }
 
-// empty(like, type, n) or empty(like, type, n, m): a tensor on the device of `like`; type: a bsp_dtype, 3 uint8, 4 int32.
+// empty(like, type, n) or empty(like, type, n, m): a tensor on the device of `like`; type: a bsp_dtype, 3 uint8, 4 int32, 5 float8_e4m3fn.
 PyObject *empty(PyObject *, PyObject *const *args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     if (n != 3 && n != 4) {
         PyErr_SetString(PyExc_TypeError, "empty(tensor, type, n[, m])");
         return nullptr;
     }
-    constexpr at::ScalarType types[] = {at::kFloat, at::kBFloat16, at::kHalf, at::kByte, at::kInt};
-    constexpr const char *names[] = {"float32", "bfloat16", "float16", "uint8", "int32"};
+    constexpr at::ScalarType types[] = {at::kFloat, at::kBFloat16, at::kHalf, at::kByte, at::kInt, at::kFloat8_e4m3fn};
+    constexpr const char *names[] = {"float32", "bfloat16", "float16", "uint8", "int32", "float8_e4m3fn"};
     const long long type = PyLong_AsLongLong(args[1]);
     int64_t size[2] = {0, 0};
     for (Py_ssize_t i = 2; i < n; ++i) size[i - 2] = PyLong_AsLongLong(args[i]);
     if (PyErr_Occurred()) return nullptr;
-    if (type < 0 || type > 4) {
+    if (type < 0 || type > 5) {
         PyErr_SetString(PyExc_ValueError, "unknown type");
         return nullptr;
     }
@@ -269,6 +270,148 @@ PyObject *last(PyObject *, PyObject *o) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- lists of tensors -----------------------------------------------------------------------------------------------------------
+struct Owned {  // a reference that ends with its scope
+    PyObject *o;
+    ~Owned() { Py_XDECREF(o); }
+};
+
+PyObject *bad_list(const char *what) {
+    PyErr_Format(PyExc_ValueError, "bsp_adamw_step: %s", what);
+    return nullptr;
+}
+
+// A plain contiguous tensor on device `device`; null with the error set.
+const at::Tensor *listed_tensor(PyObject *o, const char *name, int64_t device) {
+    if (!THPVariable_Check(o)) {
+        PyErr_Format(PyExc_TypeError, "bsp_adamw_step: %s must hold tensors, got %s", name, Py_TYPE(o)->tp_name);
+        return nullptr;
+    }
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || !t.is_contiguous() || t.device().index() != device) {
+        PyErr_Format(PyExc_ValueError, "bsp_adamw_step: %s must hold contiguous tensors on the current device", name);
+        return nullptr;
+    }
+    return &t;
+}
+
+// bsp_adamw_step(W, G, m, v, scales, copies, keep, alpha, R, weight_decay, bits, lam, lr, beta1, beta2, eps, t, seed, lr_t, grad_scale,
+// device, stream): the lists' tensors as descriptions.  (A model's 400 tensors one by one from Python would take ten times as long as their step.)
+PyObject *adamw_step(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    if (n_args != 22) {
+        PyErr_Format(PyExc_TypeError, "this function takes 22 arguments (%zd given)", n_args);
+        return nullptr;
+    }
+    constexpr const char *names[] = {"W", "G", "m", "v", "scales", "copies", "keep", "alpha"};
+    PyObject *list[8];
+    Owned owned[10] = {};
+    Py_ssize_t count = -1;
+    for (int i = 0; i < 8; ++i) {
+        list[i] = nullptr;
+        if (args[i] == Py_None && i >= 4) continue;
+        list[i] = owned[i].o = PySequence_Fast(args[i], "bsp_adamw_step takes lists of tensors");
+        if (!list[i]) return nullptr;
+        const Py_ssize_t n = PySequence_Fast_GET_SIZE(list[i]);
+        if (count < 0) count = n;
+        if (n != count) return bad_list("the lists must have one length");
+    }
+    PyObject *rows = nullptr, *decays = nullptr;  // lists, or numbers for all tensors
+    int32_t row = 0;
+    float decay = 0.0f;
+    if (PyList_Check(args[8]) || PyTuple_Check(args[8])) rows = owned[8].o = PySequence_Fast(args[8], "");
+    else if (!read_whole(args[8], row)) return nullptr;
+    if (PyList_Check(args[9]) || PyTuple_Check(args[9])) decays = owned[9].o = PySequence_Fast(args[9], "");
+    else if (!read_real(args[9], decay)) return nullptr;
+    for (PyObject *l : {rows, decays})
+        if (l && PySequence_Fast_GET_SIZE(l) != count) return bad_list("the lists must have one length");
+    int bits;
+    float real[5];
+    int64_t t, device;
+    uint64_t seed;
+    void *lr_t, *grad_scale, *stream;
+    if (!read_whole(args[10], bits)) return nullptr;
+    for (int i = 0; i < 5; ++i)
+        if (!read_real(args[11 + i], real[i])) return nullptr;
+    if (!read_whole(args[16], t) || !read_whole(args[17], seed) || !read_tensor(args[18], "float32", at::kFloat, lr_t) ||
+        !read_tensor(args[19], "float32", at::kFloat, grad_scale) || !read_whole(args[20], device))
+        return nullptr;
+    for (int i = 18; i < 20; ++i)
+        if (args[i] != Py_None && THPVariable_Check(args[i])) {
+            const at::Tensor &x = THPVariable_Unpack(args[i]);
+            if (x.device().index() != device || x.numel() < (i == 18 ? 2 : 1)) return bad_list("lr_t holds 2 and grad_scale 1 number on the current device");
+        }
+    stream = PyLong_AsVoidPtr(args[21]);
+    if (PyErr_Occurred()) return nullptr;
+
+    std::vector<bsp_adamw_tensor> tensors((size_t)count);
+    at::ScalarType gdt = at::kFloat, cdt = at::kBFloat16;
+    bool copies = false;
+    const at::ScalarType moment = bits == 8 ? at::kFloat8_e4m3fn : at::kFloat;
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        const at::Tensor *x[8];
+        for (int k = 0; k < 8; ++k) {
+            PyObject *o = list[k] ? PySequence_Fast_GET_ITEM(list[k], i) : Py_None;
+            if (o == Py_None && k >= 5) {
+                x[k] = nullptr;
+                continue;
+            }
+            if (k == 4 && !list[4]) {
+                x[4] = nullptr;
+                continue;
+            }
+            x[k] = listed_tensor(o, names[k], device);
+            if (!x[k]) return nullptr;
+        }
+        const at::Tensor &w = *x[0];
+        if (w.scalar_type() != at::kFloat) return bad_list("W must be float32");
+        if (i == 0) gdt = x[1]->scalar_type();
+        if (gdt != at::kFloat && gdt != at::kBFloat16 && gdt != at::kHalf) return bad_list("G must be float32, bfloat16 or float16");
+        if (x[1]->scalar_type() != gdt || x[1]->sizes() != w.sizes()) return bad_list("G must have the shapes of W and one dtype");
+        for (int k = 2; k < 4; ++k)
+            if (x[k]->scalar_type() != moment || x[k]->sizes() != w.sizes())
+                return bad_list("m and v must have the shapes of W and be float32, or float8_e4m3fn with scales");
+        bsp_adamw_tensor &d = tensors[(size_t)i];
+        const int64_t n = w.numel();
+        const bool grouped = x[6] || x[7];
+        d.N = grouped && w.dim() > 0 ? w.size(-1) : 1;  // (without groups the shape is of no account)
+        d.M = d.N ? n / d.N : 0;
+        d.R = row;
+        d.weight_decay = decay;
+        if (rows && !read_whole(PySequence_Fast_GET_ITEM(rows, i), d.R)) return nullptr;
+        if (decays && !read_real(PySequence_Fast_GET_ITEM(decays, i), d.weight_decay)) return nullptr;
+        if (x[4] && (x[4]->scalar_type() != at::kFloat || x[4]->numel() != 2 * ((n + 255) / 256))) return bad_list("scales must be float32, 2 for every 256 elements");
+        if (x[5]) {
+            if (!copies) cdt = x[5]->scalar_type();
+            copies = true;
+            if (x[5]->scalar_type() != cdt || (cdt != at::kBFloat16 && cdt != at::kHalf) || x[5]->sizes() != w.sizes())
+                return bad_list("copies must have the shapes of W and one 16-bit dtype");
+        }
+        if (grouped && n && (d.R <= 0 || d.M % d.R != 0)) return bad_list("a tensor with keep or alpha must have whole row-blocks of R rows");
+        if (x[6] && (x[6]->scalar_type() != at::kByte || (n && x[6]->numel() != n / d.R))) return bad_list("keep must be uint8 [M / R, N]");
+        if (x[7] && (x[7]->scalar_type() != at::kFloat || (n && x[7]->numel() != n / d.R))) return bad_list("alpha must be float32 [M / R, N]");
+        void *at[8];
+        for (int k = 0; k < 8; ++k) at[k] = x[k] ? x[k]->data_ptr() : nullptr;
+        d.w = (float *)at[0];
+        d.g = at[1];
+        d.m = at[2];
+        d.v = at[3];
+        d.scales = (float *)at[4];
+        d.copy = at[5];
+        d.keep = (const uint8_t *)at[6];
+        d.alpha = (const float *)at[7];
+    }
+    int st;
+    {
+        const Unlocked unlocked;
+        st = bsp_adamw_step(tensors.data(), count, gdt == at::kFloat ? BSP_F32 : (gdt == at::kBFloat16 ? BSP_BF16 : BSP_F16),
+                            cdt == at::kHalf ? BSP_F16 : BSP_BF16, bits, real[0], real[1], real[2], real[3], real[4], t, (uint32_t)seed,
+                            (const float *)lr_t, (const float *)grad_scale, stream);
+    }
+    return PyLong_FromLong(st);
+    END_HANDLE_TH_ERRORS
+}
+
 #define BSP_ENTRY(name, check) \
     {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&Entry<&name, check>::run)), METH_FASTCALL, nullptr}
 
@@ -292,6 +435,15 @@ PyMethodDef methods[] = {
     BSP_ENTRY(bsp_linear_plan, kNone),
     BSP_ENTRY(bsp_linear_planned, kNone),
     BSP_ENTRY(bsp_linear_planned_fused, kNone),
+    BSP_ENTRY(bsp_fp8_quant, kByte),
+    BSP_ENTRY(bsp_matmul_fp8_workspace_bytes, kNone),
+    BSP_ENTRY(bsp_matmul_fp8, kByte),
+    BSP_ENTRY(bsp_linear_fp8_workspace_bytes, kNone),
+    BSP_ENTRY(bsp_linear_fp8, kByte),
+    BSP_ENTRY(bsp_block_norm, kFloat),
+    BSP_ENTRY(bsp_block_norm_backward_workspace_bytes, kNone),
+    BSP_ENTRY(bsp_block_norm_backward, kFloat),
+    {"bsp_adamw_step", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&adamw_step)), METH_FASTCALL, nullptr},
     {"empty", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&empty)), METH_FASTCALL, nullptr},
     {"last", last, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},

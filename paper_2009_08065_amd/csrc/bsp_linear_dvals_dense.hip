@@ -31,19 +31,10 @@ __device__ __forceinline__ uint32_t dd_turn(uint32_t token) {
     return PITCH >= 256 ? (token & 3u) << 6 : ((token >> 1) & 1u) << 6;
 }
 
-// 64 lanes' 16 bytes at base + at to LDS at lds .. lds + 1023.  (Written out: for the builtin the compiler would wait for all such
-// loads before any LDS read.  m0 is a reserved register, which can't be named as clobbered; nothing else in these kernels uses it.)
-__device__ __forceinline__ void load_to_lds(uint32_t lds, const uint8_t *base, uint32_t at) {
-    asm volatile("s_mov_b32 m0, %0\n s_nop 0\n global_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(at), "s"(base));
-}
-// The same at lds + PLUS.
+// load_to_lds to lds + PLUS.
 template <int PLUS>
 __device__ __forceinline__ void load_to_lds_at(uint32_t lds, const uint8_t *base, uint32_t at) {
     asm volatile("s_add_u32 m0, %0, %3\n s_nop 0\n global_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(at), "s"(base), "n"(PLUS) : "scc");
-}
-template <int LEFT>
-__device__ __forceinline__ void wait_loads() {  // until LEFT loads are on their way
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
 }
 __device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
 

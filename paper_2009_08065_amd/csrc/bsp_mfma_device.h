@@ -60,6 +60,16 @@ __device__ __forceinline__ uint32_t cvt_pk(float a, float b) {
         return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, f16x2));
 }
 
+// 64 lanes' 16 bytes at base + at to LDS at lds .. lds + 1023.  (Written out: for the builtin the compiler would wait for all such
+// loads before any LDS read.  m0 is a reserved register, which can't be named as clobbered; nothing else in these kernels uses it.)
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const uint8_t *base, uint32_t at) {
+    asm volatile("s_mov_b32 m0, %0\n s_nop 0\n global_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(at), "s"(base));
+}
+template <int LEFT>
+__device__ __forceinline__ void wait_loads() {  // until LEFT loads are on their way
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
+}
+
 extern __shared__ __attribute__((aligned(16))) uint8_t smem_x[];
 
 // f(integral_constant<int, I>) for I = B .. E - 1: a loop whose index is a constant inside the body, so that
