@@ -644,9 +644,10 @@ def bsp_linear_fp8(X, W: Fp8, bias=None, act=0, residual=None, Y=None, ws=None):
         raise ValueError("Y must be a [T, M] tensor of the dtype of X")
     _epilogue_fits(T, W.rows, X.dtype, bias, residual)
     if ws is None:
-        ws = native.empty(X, _U8, native.bsp_linear_fp8_workspace_bytes(T, W.rows, N))
+        need = native.bsp_linear_fp8_workspace_bytes(T, W.rows, N)
+        ws = native.empty(X, _U8, need) if need else None
     st = native.bsp_linear_fp8(X, _DT[X.dtype], T, W.rows, N, W.codes, W.scales, W.layout, bias, act, residual, Y, ws,
-                               ws.numel() * ws.element_size(), _stream())
+                               0 if ws is None else ws.numel() * ws.element_size(), _stream())
     _check(st, "bsp_linear_fp8")
     return Y
 

@@ -85,20 +85,36 @@ __device__ __forceinline__ int find_tensor(const Table &tab) {
     return __builtin_popcountll(__ballot(before)) - 1;
 }
 
-// Place of an element in the group arrays [M / R, N]: rows and columns counted from the row that `base` lies in.
+// Place of an element in the group arrays [M / R, N], carried along a walk in equal strides: row-block, row in it and column.
 struct Groups {
-    int64_t row0;
-    uint32_t col0, N, R;
+    uint32_t col, row, N, R;
+    int64_t block;
     __device__ __forceinline__ Groups(const Entry &e, int64_t base) : N(e.N), R(e.R) {
-        row0 = e.n <= 0xffffffffll ? (int64_t)((uint32_t)base / N) : base / N;
-        col0 = (uint32_t)(base - row0 * N);
+        const int64_t r = e.n <= 0xffffffffll ? (int64_t)((uint32_t)base / N) : base / N;
+        block = r <= 0xffffffffll ? (int64_t)((uint32_t)r / R) : r / R;
+        col = (uint32_t)(base - r * N);
+        row = (uint32_t)(r - block * R);
     }
-    __device__ __forceinline__ int64_t at(uint32_t local) const {
-        const uint32_t c = col0 + local, q = c / N;
-        const int64_t row = row0 + q;
-        const int64_t b = row <= 0xffffffffll ? (int64_t)((uint32_t)row / R) : row / R;
-        return b * N + (c - q * N);
+    // (a division where a stride passes several rows only: divisions for every element were a third of the masked kernel's instructions)
+    __device__ __forceinline__ void advance(uint32_t stride) {
+        col += stride;
+        if (col < N) return;
+        if (N >= stride) {
+            col -= N;
+            if (++row == R) {
+                row = 0;
+                ++block;
+            }
+        } else {
+            const uint32_t q = col / N;
+            col -= q * N;
+            row += q;
+            const uint32_t b = row / R;
+            row -= b * R;
+            block += b;
+        }
     }
+    __device__ __forceinline__ int64_t at() const { return block * N + col; }
 };
 
 __device__ __forceinline__ float update(float w, float m, float v, float lr, float c1, float c2, float eps) {
@@ -124,7 +140,9 @@ __global__ __launch_bounds__(kThreads) void adamw32_kernel(Table tab, Hyper h) {
     const int64_t base = (int64_t)(blockIdx.x - tab.first[k]) * kChunk32;
     float *w = e.w + base, *m = (float *)e.m + base, *v = (float *)e.v + base;
     const int64_t left = e.n - base;
-    const Groups groups(e, base);
+    const bool grouped = e.keep || e.alpha;
+    Groups groups(e, grouped ? base : 0);
+    if (grouped) groups.advance(threadIdx.x);
     const float decay = s.lr * e.decay;
 #pragma unroll 4
     for (int j = 0; j < kPerThread; ++j) {
@@ -134,7 +152,10 @@ __global__ __launch_bounds__(kThreads) void adamw32_kernel(Table tab, Hyper h) {
         float g = elem<GDT>::load(e.g, base + i);
         if (h.grad_scale) g = g * s.gs;
         int64_t at = 0;
-        if (e.keep || e.alpha) at = groups.at(i);
+        if (grouped) {
+            at = groups.at();
+            groups.advance(kThreads);
+        }
         if (e.alpha) g = __builtin_fmaf(h.lambda * e.alpha[at], w0, g);
         const float t1 = h.beta1 * m[i];
         const float t2 = h.omb1 * g;
@@ -164,11 +185,19 @@ __device__ __forceinline__ uint32_t mix(uint32_t x) {
     return x ^ (x >> 16);
 }
 
-// The largest of 64 lanes' values (all >= 0), in every lane.
+// The largest of 64 lanes' values (all >= 0), in every lane: within rows of 16 lanes and then across them, without LDS.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float max_dpp(float x) {
+    return __builtin_fmaxf(x, __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, ROWS, 0xf, false)));
+}
 __device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) x = __builtin_fmaxf(x, __shfl_xor(x, d));
-    return x;
+    x = max_dpp<0x111, 0xf>(x);  // row_shr 1, 2, 4, 8: lane 15 of a row has the row's
+    x = max_dpp<0x112, 0xf>(x);
+    x = max_dpp<0x114, 0xf>(x);
+    x = max_dpp<0x118, 0xf>(x);
+    x = max_dpp<0x142, 0xa>(x);  // row_bcast 15 into rows 1 and 3, 31 into rows 2 and 3
+    x = max_dpp<0x143, 0xc>(x);
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), 63));
 }
 
 // |y| <= 448 to one of the two codes' values next to it, up where the 16 bits (of 2^16) exceed what is missing.  Below 2^-6 the
@@ -199,9 +228,12 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(Table tab, Hyper h) {
     const Entry &e = tab.e[k];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t base = (int64_t)(blockIdx.x - tab.first[k]) * kChunk8 + wave * (kBlocksPerWave * kBlock);
-    const Groups groups(e, base);
+    const bool grouped = e.keep || e.alpha;
+    Groups groups(e, grouped ? base : 0);
+    if (grouped) groups.advance(4 * lane);
+    const bool one_row = (e.N & 3) == 0;  // a lane's four elements are neighbours in the group arrays
     const int64_t blocks = (e.n + kBlock - 1) / kBlock;
-    const float decay = s.lr * e.decay;
+    const float decay = s.lr * e.decay, rate = s.lr / s.c1, root = 1.0f / __builtin_sqrtf(s.c2);
     uint8_t *m8 = (uint8_t *)e.m, *v8 = (uint8_t *)e.v;
     for (int b = 0; b < kBlocksPerWave; ++b) {
         const int64_t i0 = base + b * kBlock + 4 * lane, block = base / kBlock + b;
@@ -237,27 +269,47 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(Table tab, Hyper h) {
         const float sm = e.scales[block], sv = e.scales[blocks + block];
         const float m0[4] = {value_of<0>(mc), value_of<1>(mc), value_of<2>(mc), value_of<3>(mc)};
         const float r0[4] = {value_of<0>(vc), value_of<1>(vc), value_of<2>(vc), value_of<3>(vc)};
+        uint32_t kept = 0xfu;
+        float coef[4] = {0, 0, 0, 0};
+        if (grouped) {
+            Groups at = groups;
+            groups.advance(kBlock);
+            if (four && one_row) {
+                if (e.keep) {
+                    uint32_t k4;
+                    __builtin_memcpy(&k4, e.keep + at.at(), 4);
+                    kept = ((k4 & 0xffu) != 0) | ((k4 & 0xff00u) != 0) << 1 | ((k4 & 0xff0000u) != 0) << 2 | ((k4 & 0xff000000u) != 0) << 3;
+                }
+                if (e.alpha) __builtin_memcpy(coef, e.alpha + at.at(), 16);
+            } else {
+                kept = 0u;
+                for (int j = 0; j < have; ++j) {
+                    if (!e.keep || e.keep[at.at()]) kept |= 1u << j;
+                    const float c = e.alpha ? e.alpha[at.at()] : 0.0f;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) coef[k] = k == j ? c : coef[k];
+                    at.advance(1);
+                }
+            }
+        }
         float top_m = 0.0f, top_r = 0.0f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            int64_t at = 0;
-            const bool grouped = (e.keep || e.alpha) && j < have;
-            if (grouped) at = groups.at((uint32_t)(i0 + j - base));
             float x = g[j];
             if (h.grad_scale) x = x * s.gs;
-            if (grouped && e.alpha) x = __builtin_fmaf(h.lambda * e.alpha[at], w[j], x);
+            if (e.alpha) x = __builtin_fmaf(h.lambda * coef[j], w[j], x);
             m[j] = h.beta1 * (m0[j] * sm) + h.omb1 * x;
             const float ro = r0[j] * sv;
             const float v = h.beta2 * (ro * ro) + h.omb2 * x * x;
-            r[j] = __builtin_sqrtf(v);
+            // (square root and reciprocal of the instructions, 1 ulp: the moments themselves are known to a sixteenth)
+            r[j] = __builtin_amdgcn_sqrtf(v);
             float wn = w[j];
             if (decay != 0.0f) {
                 const float d = decay * wn;
                 wn = wn - d;
             }
-            wn = update(wn, m[j], v, s.lr, s.c1, s.c2, h.eps);
-            if (grouped && e.keep && !e.keep[at]) wn = 0.0f;
-            w[j] = wn;
+            wn = wn - rate * m[j] * __builtin_amdgcn_rcpf(__builtin_fmaf(r[j], root, h.eps));
+            w[j] = (kept >> j) & 1u ? wn : 0.0f;
             top_m = __builtin_fmaxf(top_m, __builtin_fabsf(m[j]));
             top_r = __builtin_fmaxf(top_r, r[j]);
         }

@@ -21,7 +21,6 @@ struct Quant {
     const void *X;
     uint8_t *Q, *S, *Qt, *St;
     int64_t rows, cols, tiles_c, pitch, pitch_t;  // pitches of Q and Qt: columns and rows, padded to 128
-    int32_t vec;
 };
 
 template <int DT, bool BLOCK, bool TRANSPOSED>
@@ -38,14 +37,8 @@ __global__ __launch_bounds__(kThreads) void quant_kernel(Quant a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int64_t at = (row0 + i) * a.cols + col0;
-        if (i < rows && cols == 8 && a.vec) {
-            if constexpr (DT == BSP_F32) {
-                const float4 p = *reinterpret_cast<const float4 *>((const float *)a.X + at);
-                const float4 q = *reinterpret_cast<const float4 *>((const float *)a.X + at + 4);
-                v[i][0] = p.x, v[i][1] = p.y, v[i][2] = p.z, v[i][3] = p.w, v[i][4] = q.x, v[i][5] = q.y, v[i][6] = q.z, v[i][7] = q.w;
-            } else {
-                unpack8<DT>(*reinterpret_cast<const uint4 *>((const uint16_t *)a.X + at), v[i]);
-            }
+        if (i < rows && cols == 8) {
+            load8<DT>(a.X, at, v[i]);
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[i][j] = i < rows && j < cols ? elem<DT>::load(a.X, at + j) : 0.0f;
@@ -155,7 +148,7 @@ extern "C" int bsp_fp8_quant(const void *X, int xdt, int64_t rows, int64_t cols,
     if (!aligned(X, dtype_size(xdt)) || !aligned(Q, 16) || !aligned(Qt, 16)) return BSP_ERR_SHAPE;
     const int64_t tiles_r = (rows + 127) / 128, tiles_c = (cols + 127) / 128;
     if (tiles_r * tiles_c >= ((int64_t)1 << 31)) return BSP_ERR_SHAPE;
-    const Quant a = {X, (uint8_t *)Q, S, (uint8_t *)Qt, St, rows, cols, tiles_c, 128 * tiles_c, 128 * tiles_r, aligned(X, 16) && cols % 8 == 0};
+    const Quant a = {X, (uint8_t *)Q, S, (uint8_t *)Qt, St, rows, cols, tiles_c, 128 * tiles_c, 128 * tiles_r};
     BSP_DISPATCH_DTYPE(xdt, DT, { launch<DT>(a, (unsigned)(tiles_r * tiles_c), layout == BSP_FP8_BLOCK, Qt != nullptr, (hipStream_t)stream); });
     return check_launch();
 }

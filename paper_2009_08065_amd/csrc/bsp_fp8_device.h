@@ -43,6 +43,18 @@ __device__ __forceinline__ void unpack8(uint4 p, float *v) {
     }
 }
 
+// Eight consecutive elements at any address (loads of 16 bytes need no alignment here).
+template <int DT>
+__device__ __forceinline__ void load8(const void *p, int64_t at, float *v) {
+    if constexpr (DT == BSP_F32) {
+        __builtin_memcpy(v, (const float *)p + at, 32);
+    } else {
+        uint4 x;
+        __builtin_memcpy(&x, (const uint16_t *)p + at, 16);
+        unpack8<DT>(x, v);
+    }
+}
+
 // Eight consecutive outputs at y: the sums v with bias, activation and residual, in fp32, rounded once.  vec: y is a multiple of 8 elements
 // from an aligned row; cols: how many there are.
 template <int DT>

@@ -231,6 +231,109 @@ __global__ __launch_bounds__(64 * WA * WB) void fp8_tile_kernel(Product p) {
     }
 }
 
+// ---- few tokens ---------------------------------------------------------------------------------------------------------------
+// Up to 16 NT tokens: B is read once and straight into registers (a wavefront's 16 rows x 128 columns are whole lines), the steps of 128
+// columns dealt to the workgroup's wavefronts in turn, whose sums meet in LDS in ascending order.  What bounds it is B's way from memory,
+// and for small matrices the launch.
+// RAW: the tokens come in XDT and are quantised here, in registers, by every workgroup for itself: 32 values of a lane, four lanes to
+// a segment.  That is less than a launch of its own for one tile of tokens.
+constexpr int kFewWaves = 8;
+
+template <int XDT>
+__device__ __forceinline__ i32x8 quantise_segment(const void *X, int64_t at, int cols, uint32_t &e) {
+    float v[32];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (cols >= 8 * (k + 1)) {
+            load8<XDT>(X, at + 8 * k, v + 8 * k);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[8 * k + j] = 8 * k + j < cols ? elem<XDT>::load(X, at + 8 * k + j) : 0.0f;
+        }
+    }
+    float m = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 32; ++k) m = __builtin_fmaxf(m, magnitude(v[k]));
+    m = __builtin_fmaxf(m, __shfl_xor(m, 16));
+    m = __builtin_fmaxf(m, __shfl_xor(m, 32));
+    e = scale_exponent(m);
+    const float s = inverse_scale(e);
+    i32x8 c;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const float y[4] = {s * v[4 * k], s * v[4 * k + 1], s * v[4 * k + 2], s * v[4 * k + 3]};
+        c[k] = (int)codes4(y);
+    }
+    return c;
+}
+
+template <int DT, int NT, bool RAW>
+__global__ __launch_bounds__(64 * kFewWaves) void fp8_few_kernel(Product p, const void *X, int64_t N) {
+    __shared__ __align__(16) float sums[kFewWaves][NT * 16][20];  // (20: a token's 16 outputs and a gap, for the banks)
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
+    const int l16 = lane & 15, quarter = lane >> 4;
+    const int64_t m0 = (int64_t)blockIdx.x * 16;
+    const int64_t row = m0 + l16 < p.M ? m0 + l16 : p.M - 1;
+    const uint8_t *b = p.B + row * p.pitch + 32 * quarter;
+    const uint8_t *sb = p.SB + (p.block ? row / 128 : row) * p.steps;
+    int64_t token[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) token[t] = 16 * t + l16 < p.T ? 16 * t + l16 : p.T - 1;
+
+    f32x4 acc[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    u32x4 next0, next1;
+    uint32_t next_e;
+    auto ask = [&](int s) {
+        next0 = *reinterpret_cast<const u32x4 *>(b + (int64_t)s * 128);
+        next1 = *reinterpret_cast<const u32x4 *>(b + (int64_t)s * 128 + 16);
+        next_e = sb[s];
+    };
+    ask(wave);  // (there are no more wavefronts than steps)
+    for (int s = wave; s < p.steps; s += waves) {
+        const u32x4 w0 = next0, w1 = next1;
+        const uint32_t es = next_e;
+        if (s + waves < p.steps) ask(s + waves);
+        const i32x8 w = {(int)w0[0], (int)w0[1], (int)w0[2], (int)w0[3], (int)w1[0], (int)w1[1], (int)w1[2], (int)w1[3]};
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            i32x8 x;
+            uint32_t e;
+            if constexpr (RAW) {
+                const int64_t k = (int64_t)s * 128 + 32 * quarter;
+                x = quantise_segment<DT>(X, token[t] * N + k, N - k > 32 ? 32 : (int)(N - k), e);
+            } else {
+                const uint8_t *a = p.A + token[t] * p.pitch + (int64_t)s * 128 + 32 * quarter;
+                const u32x4 x0 = *reinterpret_cast<const u32x4 *>(a), x1 = *reinterpret_cast<const u32x4 *>(a + 16);
+                x = i32x8{(int)x0[0], (int)x0[1], (int)x0[2], (int)x0[3], (int)x1[0], (int)x1[1], (int)x1[2], (int)x1[3]};
+                e = p.SA[token[t] * p.steps + s];
+            }
+            if constexpr (DT == BSP_F32) {
+#pragma unroll
+                for (int k = 0; k < 8; k += 2)
+                    acc[t] = mfma16<BSP_BF16>(widen8((uint32_t)w[k], (uint32_t)w[k + 1], es), widen8((uint32_t)x[k], (uint32_t)x[k + 1], e), acc[t]);
+            } else {
+                acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc[t], 0, 0, 0, (int)es, 0, (int)e);
+            }
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4 *>(&sums[wave][16 * t + l16][4 * quarter]) = acc[t];
+    __syncthreads();
+    for (int i = tid; i < NT * 256; i += blockDim.x) {
+        const int t = i >> 4, c = i & 15;
+        const int64_t m = m0 + c;
+        if (t >= p.T || m >= p.M) continue;
+        float v = 0.0f;
+        for (int w = 0; w < waves; ++w) v += sums[w][t][c];
+        if (p.bias) v += elem<DT>::load(p.bias, m);
+        if (p.act == BSP_ACT_GELU) v = gelu_fit(v);
+        if (p.residual) v += elem<DT>::load(p.residual, t * p.M + m);
+        elem<DT>::store(p.Y, t * p.M + m, v);
+    }
+}
+
 // The splits' sums, ascending, then bias, activation and residual.
 template <int DT>
 __global__ __launch_bounds__(256) void fp8_join_kernel(Product p, int splits) {
@@ -253,14 +356,20 @@ __global__ __launch_bounds__(256) void fp8_join_kernel(Product p, int splits) {
     finish8<DT>(v, bias, p.act, p.residual, p.Y, t * p.M + m, (p.M & 7) == 0, cols);
 }
 
-// 1 where the product is not split.
+constexpr int64_t kFewTokens = 64;  // of fp8_few_kernel
+constexpr int64_t kRawTokens = 16;  // quantised by every workgroup
+
 struct Shape {
-    int tile;    // 256, 128 or 64
+    int tile;    // 256, 128 or 64; 0: few tokens
     int splits, split_steps;
 };
 
 Shape choose(int64_t T, int64_t M, int64_t steps) {
     Shape s = {256, 1, (int)steps};
+    if (T <= kFewTokens) {
+        s.tile = 0;
+        return s;
+    }
     auto count = [&](int64_t t) { return ((T + t - 1) / t) * ((M + t - 1) / t); };
     if (count(256) < 192) s.tile = 128;
     if (s.tile == 128 && count(128) < 192) s.tile = 64;
@@ -294,9 +403,23 @@ int launch_tile(const Product &p, int splits, hipStream_t s) {
     return check_launch();
 }
 
+template <int DT, bool RAW>
+int launch_few(const Product &p, const void *X, int64_t N, hipStream_t s) {
+    const unsigned grid = (unsigned)((p.M + 15) / 16), threads = 64u * (unsigned)(p.steps < kFewWaves ? p.steps : kFewWaves);
+    if constexpr (RAW) {
+        fp8_few_kernel<DT, 1, true><<<grid, threads, 0, s>>>(p, X, N);
+    } else {
+        if (p.T <= 16) fp8_few_kernel<DT, 1, false><<<grid, threads, 0, s>>>(p, X, N);
+        else if (p.T <= 32) fp8_few_kernel<DT, 2, false><<<grid, threads, 0, s>>>(p, X, N);
+        else fp8_few_kernel<DT, 4, false><<<grid, threads, 0, s>>>(p, X, N);
+    }
+    return check_launch();
+}
+
 template <int DT>
 int launch_product(const Product &p, const Shape &c, hipStream_t s) {
     int st;
+    if (c.tile == 0) return launch_few<DT, false>(p, nullptr, 0, s);
     if (c.tile == 256) st = launch_tile<DT, 2, 4, 4, 2>(p, c.splits, s);
     else if (c.tile == 128) st = launch_tile<DT, 2, 2, 2, 2>(p, c.splits, s);
     else st = launch_tile<DT, 1, 1, 2, 2>(p, c.splits, s);
@@ -356,6 +479,7 @@ extern "C" int bsp_matmul_fp8(const void *A, const uint8_t *SA, const void *B, c
 
 extern "C" size_t bsp_linear_fp8_workspace_bytes(int64_t T, int64_t M, int64_t N) {
     if (T <= 0 || check_sizes(T, M, N, BSP_FP8_ROW, BSP_F32, BSP_ACT_NONE)) return 0;
+    if (T <= kRawTokens) return 0;
     return up256((size_t)T * 128 * steps_of(N)) + up256((size_t)T * steps_of(N)) + split_bytes(T, M, N);
 }
 
@@ -363,10 +487,20 @@ extern "C" int bsp_linear_fp8(const void *X, int xdt, int64_t T, int64_t M, int6
                               const void *bias, int act, const void *residual, void *Y, void *ws, size_t ws_bytes, void *stream) {
     if (int st = check_sizes(T, M, N, w_layout, xdt, act)) return st;
     if (T == 0) return BSP_OK;
-    if (!X || !W || !SW || !Y || !ws) return BSP_ERR_NULL;
+    const bool raw = T <= kRawTokens;
+    if (!X || !W || !SW || !Y || (!raw && !ws)) return BSP_ERR_NULL;
     const size_t size = dtype_size(xdt);
     if (!aligned(X, size) || !aligned(W, 16) || !aligned(Y, size) || !aligned(bias, size) || !aligned(residual, size) || !aligned(ws, 256)) return BSP_ERR_SHAPE;
     if (ws_bytes < bsp_linear_fp8_workspace_bytes(T, M, N)) return BSP_ERR_CAPACITY;
+    if (raw) {
+        const Product p = {nullptr, nullptr, (const uint8_t *)W, SW, bias, residual, Y, nullptr, T, M, (int32_t)steps_of(N), (int32_t)(128 * steps_of(N)), 0,
+                           w_layout == BSP_FP8_BLOCK, act};
+        switch (xdt) {
+            case BSP_F32: return launch_few<BSP_F32, true>(p, X, N, (hipStream_t)stream);
+            case BSP_BF16: return launch_few<BSP_BF16, true>(p, X, N, (hipStream_t)stream);
+            default: return launch_few<BSP_F16, true>(p, X, N, (hipStream_t)stream);
+        }
+    }
     uint8_t *codes = (uint8_t *)ws, *scales = codes + up256((size_t)T * 128 * steps_of(N)), *rest = scales + up256((size_t)T * steps_of(N));
     if (int st = bsp_fp8_quant(X, xdt, T, N, BSP_FP8_ROW, codes, scales, nullptr, nullptr, stream)) return st;
     return product(codes, scales, W, SW, w_layout, T, M, N, bias, act, residual, Y, xdt, rest, split_bytes(T, M, N), (hipStream_t)stream);

@@ -140,7 +140,7 @@ def test_matmul_rows_behind_the_last_and_padding():
         assert torch.equal(y, bsp.bsp_matmul_fp8(A, B, out_dtype=dt))
 
 
-@pytest.mark.parametrize("T,M,K", [(64, 64, 8192), (200, 130, 4096), (1, 64, 16384)])
+@pytest.mark.parametrize("T,M,K", [(100, 64, 8192), (200, 130, 4096), (70, 64, 16384)])
 def test_matmul_split(T, M, K):
     """Products of few outputs and many columns, with the scratch (the columns split) and without."""
     a, b = rand(7, T, K), rand(8, M, K)

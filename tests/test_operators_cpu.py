@@ -36,15 +36,15 @@ def test_fp8_refusals():
     assert mm(A=C.c_void_p(4104)) == SHAPE and mm(B=C.c_void_p(4104)) == SHAPE and mm(Y=ODD) == SHAPE and mm(bias=ODD) == SHAPE
     assert mm(res=ODD) == SHAPE and mm(ws=C.c_void_p(4100), n=64) == SHAPE and mm(Y=C.c_void_p(4098), ydt=0) == SHAPE
     assert mm(T=0) == OK
-    need = L.bsp_matmul_fp8_workspace_bytes(64, 64, 8192)
-    assert need > 0 and mm(T=64, M=64, K=8192, ws=P, n=need - 1) == CAP
+    need = L.bsp_matmul_fp8_workspace_bytes(100, 64, 8192)
+    assert need > 0 and mm(T=100, M=64, K=8192, ws=P, n=need - 1) == CAP
     assert L.bsp_matmul_fp8_workspace_bytes(0, 64, 64) == 0 and L.bsp_matmul_fp8_workspace_bytes(4, 0, 64) == 0
 
-    def lin(X=P, xdt=1, T=4, M=8, N=128, W=P, SW=P, lay=1, bias=None, act=0, res=None, Y=P, ws=P, n=1 << 20):
+    def lin(X=P, xdt=1, T=40, M=8, N=128, W=P, SW=P, lay=1, bias=None, act=0, res=None, Y=P, ws=P, n=1 << 20):
         return L.bsp_linear_fp8(X, xdt, T, M, N, W, SW, lay, bias, act, res, Y, ws, n, None)
     assert lin(X=None) == NULL and lin(W=None) == NULL and lin(SW=None) == NULL and lin(Y=None) == NULL and lin(ws=None) == NULL
     assert lin(xdt=9) == DTYPE and lin(lay=-1) == DTYPE and lin(N=0) == SHAPE and lin(X=ODD) == SHAPE and lin(ws=C.c_void_p(4100)) == SHAPE
-    assert lin(n=L.bsp_linear_fp8_workspace_bytes(4, 8, 128) - 1) == CAP and lin(T=0) == OK
+    assert lin(n=L.bsp_linear_fp8_workspace_bytes(40, 8, 128) - 1) == CAP and lin(T=0) == OK
 
 
 def test_block_norm_refusals():
