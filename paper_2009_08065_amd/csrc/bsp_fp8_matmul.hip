@@ -28,25 +28,13 @@ struct Product {
     const uint8_t *A, *SA, *B, *SB;
     const void *bias, *residual;
     void *Y;
-    float *partial;  // [splits][T][M] where the columns are split, else null
+    float *partial;  // [splits][T][M up to a multiple of 8] where the columns are split, else null
     int64_t T, M;
     int32_t steps, pitch, split_steps;  // steps of 128 columns; bytes of a row; steps of a split
     int32_t block, act;                 // B has a scale per 128 rows
 };
 
 __device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
-
-// Four scales at index i of an array of `total`, read as one word where it is inside; the bytes past the end are of no interest.
-__device__ __forceinline__ uint32_t scales4(const uint8_t *s, int64_t i, int64_t total) {
-    uint32_t v = 0;
-    if (i + 4 <= total) {
-        __builtin_memcpy(&v, s + i, 4);
-    } else {
-        for (int k = 0; k < 3; ++k)
-            if (i + k < total) v |= (uint32_t)s[i + k] << (8 * k);
-    }
-    return v;
-}
 
 __device__ __forceinline__ f32x16 mfma_scaled(i32x8 a, i32x8 b, f32x16 c, uint32_t sa, uint32_t sb) {
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, (int)sa, 0, (int)sb);
@@ -64,11 +52,11 @@ __device__ __forceinline__ uint4 widen8(uint32_t lo, uint32_t hi, uint32_t scale
 // The tile's place: workgroup ids go round the 8 XCDs; each XCD owns whole groups of kGroup token tiles and walks their output ranges.
 constexpr uint32_t kGroup = 4;
 
-template <int DT, int FA, int FB, int WA, int WB>
+template <int DT, int FA, int FB, int WA, int WB, int NS>
 __global__ __launch_bounds__(64 * WA * WB) void fp8_tile_kernel(Product p) {
     constexpr int kWaves = WA * WB, kThreads = 64 * kWaves;
     constexpr int TA = 32 * FA * WA, TB = 32 * FB * WB;  // outputs, tokens
-    constexpr int kStage = (TA + TB) * 128, kLoads = (TA + TB) / 8 / kWaves;
+    constexpr int kCodes = (TA + TB) * 128, kStage = kCodes + (TA + TB) * 4, kLoads = (TA + TB) / 8 / kWaves;
     constexpr int kPitch = TA + 4;  // floats of a token's row in the output pass
     static_assert((TA + TB) / 8 % kWaves == 0);
     extern __shared__ __align__(16) uint8_t smem[];
@@ -95,35 +83,23 @@ __global__ __launch_bounds__(64 * WA * WB) void fp8_tile_kernel(Product p) {
         const uint32_t row = r < left ? r : (uint32_t)(left - 1);
         at[i] = row * (uint32_t)p.pitch + ((((uint32_t)lane & 7) ^ ((r >> 1) & 7)) << 4);
     }
+    // and 64 rows' scales, one of (TA + TB) / 64 pieces (in tiles of fewer rows than lanes several wavefronts load the same piece)
+    constexpr int kScalePieces = (TA + TB) / 64;
+    static_assert(TA % 64 == 0 && TB % 64 == 0 && kScalePieces <= kWaves);
+    const int piece = wave % kScalePieces, piece_op = 64 * piece >= TA, piece_r = 64 * piece + lane - (piece_op ? TA : 0);
+    const int64_t piece_row0 = piece_op ? t0 : m0, piece_left = (piece_op ? p.T : p.M) - piece_row0;
+    const int64_t piece_row = piece_r < piece_left ? piece_r : piece_left - 1;
+    const bool blocks = !piece_op && p.block;
+    const uint8_t *scale_base = piece_op ? p.SA + t0 * p.steps : p.SB + (blocks ? m0 / 128 : m0) * p.steps;
+    const uint32_t scale_at = (uint32_t)(blocks ? (m0 + piece_row) / 128 - m0 / 128 : piece_row) * (uint32_t)p.steps;
     auto load = [&](int step, int slot) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int r8 = wave * kLoads + i, op = 8 * r8 >= TA;
             load_to_lds(slot * kStage + r8 * 1024, base[op] + (int64_t)step * 128, at[i]);
         }
+        load_bytes_to_lds(slot * kStage + kCodes + piece * 256, scale_base + step, scale_at);
     };
-    // scales: of the lane's row of each piece, four steps to a word
-    const int64_t rows_b = p.block ? (p.M + 127) / 128 : p.M, total_a = p.T * p.steps, total_b = rows_b * p.steps;
-    int64_t s_at[FA + FB];
-#pragma unroll
-    for (int f = 0; f < FA; ++f) {
-        int64_t r = m0 + wa * 32 * FA + 32 * f + l32;
-        if (r >= p.M) r = p.M - 1;
-        s_at[f] = (p.block ? r / 128 : r) * p.steps;
-    }
-#pragma unroll
-    for (int f = 0; f < FB; ++f) {
-        int64_t r = t0 + wb * 32 * FB + 32 * f + l32;
-        if (r >= p.T) r = p.T - 1;
-        s_at[FA + f] = r * p.steps;
-    }
-    uint32_t sc[FA + FB], next[FA + FB];
-    auto ask_scales = [&](int step) {
-#pragma unroll
-        for (int f = 0; f < FA + FB; ++f)
-            next[f] = step < last ? scales4(f < FA ? p.SB : p.SA, s_at[f] + step, f < FA ? total_b : total_a) : 0u;
-    };
-
     f32x16 acc[FA][FB];
 #pragma unroll
     for (int i = 0; i < FA; ++i)
@@ -140,24 +116,21 @@ __global__ __launch_bounds__(64 * WA * WB) void fp8_tile_kernel(Product p) {
         return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
     };
 
-    ask_scales(first);
-    load(first, 0);
+    static_for<0, NS - 1>([&](auto n) {
+        if (first + n < last) load(first + n, n);  // uniform
+    });
+    const uint32_t scale_a = kCodes + (uint32_t)(wa * FA * 32 + l32) * 4, scale_b = kCodes + (uint32_t)(TA + wb * FB * 32 + l32) * 4;
+    int slot = 0;
     for (int s = first; s < last; ++s) {
-        const int slot = (s - first) & 1;
-        wait_loads<0>();
-        barrier();  // this step is in LDS, and nobody reads the other slot any more
-        if (((s - first) & 3) == 0) {
+        // this step's loads are done where no more are left than those of the NS - 2 steps behind it; at the end there are fewer
+        if (NS > 2 && s + NS - 1 < last + 1) wait_loads<(NS - 2) * (kLoads + 1)>();
+        else wait_loads<0>();
+        barrier();  // this step is in LDS, and nobody reads the slot before it any more
+        if (s + NS - 1 < last) load(s + NS - 1, slot == 0 ? NS - 1 : slot - 1);
+        uint32_t sc[FA + FB];
 #pragma unroll
-            for (int f = 0; f < FA + FB; ++f) {
-                sc[f] = next[f];
-                asm volatile("" : "+v"(sc[f]));  // (waited for here, before the next loads are on their way)
-            }
-            ask_scales(s + 4);
-        } else {
-#pragma unroll
-            for (int f = 0; f < FA + FB; ++f) sc[f] >>= 8;
-        }
-        if (s + 1 < last) load(s + 1, slot ^ 1);
+        for (int f = 0; f < FA + FB; ++f)
+            sc[f] = *reinterpret_cast<const uint32_t *>(smem + slot * kStage + (f < FA ? scale_a + 128 * f : scale_b + 128 * (f - FA)));
 #pragma unroll
         for (int sub = 0; sub < 2; ++sub) {
             i32x8 a[FA], b[FB];
@@ -170,9 +143,9 @@ __global__ __launch_bounds__(64 * WA * WB) void fp8_tile_kernel(Product p) {
                     constexpr int k = 2 * decltype(kk)::value;
                     uint4 wa8[FA], wb8[FB];
 #pragma unroll
-                    for (int i = 0; i < FA; ++i) wa8[i] = widen8((uint32_t)a[i][k], (uint32_t)a[i][k + 1], sc[i] & 0xffu);
+                    for (int i = 0; i < FA; ++i) wa8[i] = widen8((uint32_t)a[i][k], (uint32_t)a[i][k + 1], sc[i]);
 #pragma unroll
-                    for (int j = 0; j < FB; ++j) wb8[j] = widen8((uint32_t)b[j][k], (uint32_t)b[j][k + 1], sc[FA + j] & 0xffu);
+                    for (int j = 0; j < FB; ++j) wb8[j] = widen8((uint32_t)b[j][k], (uint32_t)b[j][k + 1], sc[FA + j]);
 #pragma unroll
                     for (int i = 0; i < FA; ++i)
 #pragma unroll
@@ -186,6 +159,7 @@ __global__ __launch_bounds__(64 * WA * WB) void fp8_tile_kernel(Product p) {
             }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        slot = slot == NS - 1 ? 0 : slot + 1;
     }
 
     // A pass of 32 WB tokens: sums to LDS, then whole rows leave with bias, activation and residual
@@ -219,10 +193,9 @@ __global__ __launch_bounds__(64 * WA * WB) void fp8_tile_kernel(Product p) {
                 for (int n = 0; n < 4; ++n) v[4 * k + n] = x[n];
             }
             if (p.partial) {
-                float *y = p.partial + ((int64_t)blockIdx.y * p.T + t) * p.M + m;
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (k < cols) y[k] = v[k];
+                float *y = p.partial + ((int64_t)blockIdx.y * p.T + t) * ((p.M + 7) / 8 * 8) + m;
+                *reinterpret_cast<float4 *>(y) = make_float4(v[0], v[1], v[2], v[3]);
+                *reinterpret_cast<float4 *>(y + 4) = make_float4(v[4], v[5], v[6], v[7]);
                 continue;
             }
             const int64_t y = t * p.M + m;
@@ -337,8 +310,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void fp8_few_kernel(Product p, cons
 // The splits' sums, ascending, then bias, activation and residual.
 template <int DT>
 __global__ __launch_bounds__(256) void fp8_join_kernel(Product p, int splits) {
-    const int64_t per_row = (p.M + 7) / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t t = i / per_row, m = (i - t * per_row) * 8;
+    const uint32_t per_row = (uint32_t)((p.M + 7) / 8), i = blockIdx.x * 256u + threadIdx.x;
+    const uint32_t t = i / per_row, m = (i - t * per_row) * 8;
     if (t >= p.T) return;
     const int cols = p.M - m > 8 ? 8 : (int)(p.M - m);
     float v[8], bias[8];
@@ -347,13 +320,14 @@ __global__ __launch_bounds__(256) void fp8_join_kernel(Product p, int splits) {
         v[k] = 0.0f;
         bias[k] = p.bias && k < cols ? elem<DT>::load(p.bias, m + k) : 0.0f;
     }
+    const float *x = p.partial + (int64_t)i * 8;
+    const int64_t stride = p.T * per_row * 8;
+#pragma unroll 4
     for (int s = 0; s < splits; ++s) {
-        const float *x = p.partial + ((int64_t)s * p.T + t) * p.M + m;
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (k < cols) v[k] += x[k];
+        const float4 a = *reinterpret_cast<const float4 *>(x + s * stride), b = *reinterpret_cast<const float4 *>(x + s * stride + 4);
+        v[0] += a.x, v[1] += a.y, v[2] += a.z, v[3] += a.w, v[4] += b.x, v[5] += b.y, v[6] += b.z, v[7] += b.w;
     }
-    finish8<DT>(v, bias, p.act, p.residual, p.Y, t * p.M + m, (p.M & 7) == 0, cols);
+    finish8<DT>(v, bias, p.act, p.residual, p.Y, (int64_t)t * p.M + m, (p.M & 7) == 0, cols);
 }
 
 constexpr int64_t kFewTokens = 64;  // of fp8_few_kernel
@@ -385,11 +359,11 @@ Shape choose(int64_t T, int64_t M, int64_t steps) {
     return s;
 }
 
-template <int DT, int FA, int FB, int WA, int WB>
+template <int DT, int FA, int FB, int WA, int WB, int NS>
 int launch_tile(const Product &p, int splits, hipStream_t s) {
     constexpr int TA = 32 * FA * WA, TB = 32 * FB * WB;
-    constexpr size_t stages = 2 * (size_t)(TA + TB) * 128, out = (size_t)32 * WB * (TA + 4) * 4, lds = stages > out ? stages : out;
-    auto k = fp8_tile_kernel<DT, FA, FB, WA, WB>;
+    constexpr size_t stages = NS * (size_t)(TA + TB) * 132, out = (size_t)32 * WB * (TA + 4) * 4, lds = stages > out ? stages : out;
+    auto k = fp8_tile_kernel<DT, FA, FB, WA, WB, NS>;
     if (lds > 65536) {  // (asking again is harmless)
         hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) {
@@ -420,9 +394,9 @@ template <int DT>
 int launch_product(const Product &p, const Shape &c, hipStream_t s) {
     int st;
     if (c.tile == 0) return launch_few<DT, false>(p, nullptr, 0, s);
-    if (c.tile == 256) st = launch_tile<DT, 2, 4, 4, 2>(p, c.splits, s);
-    else if (c.tile == 128) st = launch_tile<DT, 2, 2, 2, 2>(p, c.splits, s);
-    else st = launch_tile<DT, 1, 1, 2, 2>(p, c.splits, s);
+    if (c.tile == 256) st = launch_tile<DT, 2, 4, 4, 2, 2>(p, c.splits, s);
+    else if (c.tile == 128) st = launch_tile<DT, 2, 2, 2, 2, 2>(p, c.splits, s);
+    else st = launch_tile<DT, 1, 1, 2, 2, 4>(p, c.splits, s);
     if (st || c.splits == 1) return st;
     const int64_t n = p.T * ((p.M + 7) / 8);
     fp8_join_kernel<DT><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(p, c.splits);
@@ -432,9 +406,13 @@ int launch_product(const Product &p, const Shape &c, hipStream_t s) {
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 int64_t steps_of(int64_t K) { return (K + 127) / 128; }
 
+size_t partial_bytes(const Shape &c, int64_t T, int64_t M) {
+    return c.splits > 1 ? (size_t)c.splits * (size_t)T * (size_t)((M + 7) / 8 * 8) * 4 : 0;
+}
+
 size_t split_bytes(int64_t T, int64_t M, int64_t K) {
     const Shape c = choose(T, M, steps_of(K));
-    return c.splits > 1 ? (size_t)c.splits * (size_t)T * (size_t)M * 4 : 0;
+    return partial_bytes(c, T, M);
 }
 
 int check_sizes(int64_t T, int64_t M, int64_t K, int layout, int ydt, int act) {
@@ -446,7 +424,7 @@ int check_sizes(int64_t T, int64_t M, int64_t K, int layout, int ydt, int act) {
 int product(const void *A, const uint8_t *SA, const void *B, const uint8_t *SB, int layout, int64_t T, int64_t M, int64_t K, const void *bias,
             int act, const void *residual, void *Y, int ydt, void *ws, size_t ws_bytes, hipStream_t s) {
     Shape c = choose(T, M, steps_of(K));
-    if (c.splits > 1 && ws_bytes < (size_t)c.splits * (size_t)T * (size_t)M * 4) c.splits = 1, c.split_steps = (int)steps_of(K);
+    if (ws_bytes < partial_bytes(c, T, M)) c.splits = 1, c.split_steps = (int)steps_of(K);
     const Product p = {(const uint8_t *)A, SA, (const uint8_t *)B, SB, bias, residual, Y, c.splits > 1 ? (float *)ws : nullptr, T, M,
                        (int32_t)steps_of(K), (int32_t)(128 * steps_of(K)), c.split_steps, layout == BSP_FP8_BLOCK, act};
     switch (ydt) {

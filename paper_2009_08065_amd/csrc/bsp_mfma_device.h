@@ -65,6 +65,10 @@ __device__ __forceinline__ uint32_t cvt_pk(float a, float b) {
 __device__ __forceinline__ void load_to_lds(uint32_t lds, const uint8_t *base, uint32_t at) {
     asm volatile("s_mov_b32 m0, %0\n s_nop 0\n global_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(at), "s"(base));
 }
+// 64 lanes' bytes at base + at to LDS as 32-bit words at lds .. lds + 255.
+__device__ __forceinline__ void load_bytes_to_lds(uint32_t lds, const uint8_t *base, uint32_t at) {
+    asm volatile("s_mov_b32 m0, %0\n s_nop 0\n global_load_lds_ubyte %1, %2" ::"s"(lds), "v"(at), "s"(base));
+}
 template <int LEFT>
 __device__ __forceinline__ void wait_loads() {  // until LEFT loads are on their way
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
