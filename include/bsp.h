@@ -462,8 +462,8 @@ int bsp_block_norm_backward(const void *dZ, const void *dH, const void *Z, const
  * aligned, undefined before and after; with NULL the call does without, slower.
  *
  * bsp_linear_fp8: the layer on X [T, N] of type xdt and quantised W [M, N]: bsp_fp8_quant of X and bsp_matmul_fp8 in one call,
- * the same bits; bias, residual and Y have type xdt.  ws: bsp_linear_fp8_workspace_bytes(T, M, N) bytes (0 for up to 16
- * tokens), 256-byte aligned.
+ * the same bits; bias, residual and Y have type xdt.  ws: bsp_linear_fp8_workspace_bytes(T, M, N) bytes (0 where few
+ * tokens are quantised on the way), 256-byte aligned.
  *
  * rows, T may be 0 (nothing is done); K <= 2^23.  Errors: BSP_ERR_NULL, BSP_ERR_DTYPE (types, layout, act), BSP_ERR_SHAPE (sizes,
  * A, B, Q, Qt not 16-byte aligned, others not by their element), BSP_ERR_CAPACITY (ws_bytes too small). */

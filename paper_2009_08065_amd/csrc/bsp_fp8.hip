@@ -6,7 +6,7 @@
 // scales there, and a code times its scale has no rounding of its own.  Against a scale of largest / 448 it leaves at most one of the
 // type's 18 binades unused.
 //
-// Bound by memory: a workgroup reads a 128 x 128 tile once, 8 x 8 values per thread, and has from it the row segments, the column
+// Bound by memory.  Row segments alone: 16 lanes to a segment.  Else a workgroup reads a 128 x 128 tile once, 8 x 8 values per thread, and has from it the row segments, the column
 // segments (the rows of the transposed matrix) or the block, and the codes of either orientation; the transposed ones go through LDS.
 #include "bsp_common.h"
 #include "bsp_fp8_device.h"
@@ -23,6 +23,63 @@ struct Quant {
     int64_t rows, cols, tiles_c, pitch, pitch_t;  // pitches of Q and Qt: columns and rows, padded to 128
 };
 
+// Eight values of a row as they came.
+template <int DT>
+struct Piece {
+    uint4 raw[DT == BSP_F32 ? 2 : 1];
+    __device__ __forceinline__ void load(const void *X, int64_t at, int cols) {
+        if (cols >= 8) {
+            __builtin_memcpy(raw, (const uint8_t *)X + at * (DT == BSP_F32 ? 4 : 2), sizeof(raw));  // (loads need no alignment here)
+        } else {
+            typename elem<DT>::type v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = j < cols ? ((const typename elem<DT>::type *)X)[at + j] : typename elem<DT>::type(0);
+            __builtin_memcpy(raw, v, sizeof(raw));
+        }
+    }
+    __device__ __forceinline__ float operator[](int j) const {
+        if constexpr (DT == BSP_F32) {
+            const uint32_t w[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
+            return __uint_as_float(w[j]);
+        } else {
+            const uint32_t w[4] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w};
+            const uint16_t h = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+            return elem<DT>::load(&h, 0);
+        }
+    }
+};
+
+// One row segment per 16 lanes, kRowsEach of them in a column of segments, all asked for at once.
+constexpr int kRowsEach = 2;
+
+template <int DT>
+__global__ __launch_bounds__(kThreads) void quant_rows_kernel(Quant a) {
+    const int c0 = 8 * (threadIdx.x & 15);
+    const int64_t strips = (a.rows + kRowsEach * 16 - 1) / (kRowsEach * 16), tc = blockIdx.x / strips, strip = blockIdx.x - tc * strips;
+    const int64_t row0 = strip * (kRowsEach * 16) + (threadIdx.x >> 4), col0 = 128 * tc + c0;
+    const int cols = a.cols - col0 > 8 ? 8 : (int)(a.cols - col0);
+    Piece<DT> v[kRowsEach];
+#pragma unroll
+    for (int i = 0; i < kRowsEach; ++i) v[i].load(a.X, (row0 + 16 * i) * a.cols + col0, row0 + 16 * i < a.rows ? cols : 0);
+#pragma unroll
+    for (int i = 0; i < kRowsEach; ++i) {
+        const int64_t row = row0 + 16 * i;
+        float m = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = __builtin_fmaxf(m, magnitude(v[i][j]));
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d));
+        if (row >= a.rows) continue;
+        const uint32_t e = scale_exponent(m);
+        const float s = inverse_scale(e);
+        float y[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = s * v[i][j];
+        *reinterpret_cast<uint2 *>(a.Q + row * a.pitch + col0) = make_uint2(codes4(y), codes4(y + 4));
+        if ((threadIdx.x & 15) == 0) a.S[row * a.tiles_c + tc] = (uint8_t)e;
+    }
+}
+
 template <int DT, bool BLOCK, bool TRANSPOSED>
 __global__ __launch_bounds__(kThreads) void quant_kernel(Quant a) {
     __shared__ float top[TRANSPOSED ? 4 * 128 : 4];
@@ -33,17 +90,9 @@ __global__ __launch_bounds__(kThreads) void quant_kernel(Quant a) {
     const int64_t row0 = 128 * tr + r0, col0 = 128 * tc + c0;
     const int rows = a.rows - row0 > 8 ? 8 : (int)(a.rows - row0), cols = a.cols - col0 > 8 ? 8 : (int)(a.cols - col0);  // (may be negative)
 
-    float v[8][8];
+    Piece<DT> v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int64_t at = (row0 + i) * a.cols + col0;
-        if (i < rows && cols == 8) {
-            load8<DT>(a.X, at, v[i]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = i < rows && j < cols ? elem<DT>::load(a.X, at + j) : 0.0f;
-        }
-    }
+    for (int i = 0; i < 8; ++i) v[i].load(a.X, (row0 + i) * a.cols + col0, i < rows ? cols : 0);
 
     uint32_t e_row[8], e_col[8];  // biased exponents of the rows' and the columns' scales
     if constexpr (BLOCK) {
@@ -127,11 +176,11 @@ __global__ __launch_bounds__(kThreads) void quant_kernel(Quant a) {
 }
 
 template <int DT>
-void launch(const Quant &a, unsigned grid, bool block, bool transposed, hipStream_t s) {
+void launch(const Quant &a, unsigned grid, int64_t rows_grid, bool block, bool transposed, hipStream_t s) {
     if (block && transposed) quant_kernel<DT, true, true><<<grid, kThreads, 0, s>>>(a);
     else if (block) quant_kernel<DT, true, false><<<grid, kThreads, 0, s>>>(a);
     else if (transposed) quant_kernel<DT, false, true><<<grid, kThreads, 0, s>>>(a);
-    else quant_kernel<DT, false, false><<<grid, kThreads, 0, s>>>(a);
+    else quant_rows_kernel<DT><<<(unsigned)rows_grid, kThreads, 0, s>>>(a);
 }
 
 }  // namespace
@@ -147,8 +196,9 @@ extern "C" int bsp_fp8_quant(const void *X, int xdt, int64_t rows, int64_t cols,
     if (!X || (Q && !S) || (Qt && !St)) return BSP_ERR_NULL;
     if (!aligned(X, dtype_size(xdt)) || !aligned(Q, 16) || !aligned(Qt, 16)) return BSP_ERR_SHAPE;
     const int64_t tiles_r = (rows + 127) / 128, tiles_c = (cols + 127) / 128;
-    if (tiles_r * tiles_c >= ((int64_t)1 << 31)) return BSP_ERR_SHAPE;
+    const int64_t rows_grid = tiles_c * ((rows + kRowsEach * 16 - 1) / (kRowsEach * 16));
+    if (rows_grid >= ((int64_t)1 << 31)) return BSP_ERR_SHAPE;
     const Quant a = {X, (uint8_t *)Q, S, (uint8_t *)Qt, St, rows, cols, tiles_c, 128 * tiles_c, 128 * tiles_r};
-    BSP_DISPATCH_DTYPE(xdt, DT, { launch<DT>(a, (unsigned)(tiles_r * tiles_c), layout == BSP_FP8_BLOCK, Qt != nullptr, (hipStream_t)stream); });
+    BSP_DISPATCH_DTYPE(xdt, DT, { launch<DT>(a, (unsigned)(tiles_r * tiles_c), rows_grid, layout == BSP_FP8_BLOCK, Qt != nullptr, (hipStream_t)stream); });
     return check_launch();
 }

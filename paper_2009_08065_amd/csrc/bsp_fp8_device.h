@@ -85,6 +85,19 @@ __device__ __forceinline__ void finish8(float (&v)[8], const float (&bias)[8], i
         } else {
             store_y16(o, make_uint4(cvt_pk<DT>(v[0], v[1]), cvt_pk<DT>(v[2], v[3]), cvt_pk<DT>(v[4], v[5]), cvt_pk<DT>(v[6], v[7])));
         }
+    } else if (cols == 8) {  // (loads and stores need no alignment)
+        if (residual) {
+            float x[8];
+            load8<DT>(r, 0, x);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] += x[k];
+        }
+        if constexpr (DT == BSP_F32) {
+            __builtin_memcpy(o, v, 32);
+        } else {
+            const uint4 x = make_uint4(cvt_pk<DT>(v[0], v[1]), cvt_pk<DT>(v[2], v[3]), cvt_pk<DT>(v[4], v[5]), cvt_pk<DT>(v[6], v[7]));
+            __builtin_memcpy(o, &x, 16);
+        }
     } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k)

@@ -83,22 +83,28 @@ __global__ __launch_bounds__(64 * WA * WB) void fp8_tile_kernel(Product p) {
         const uint32_t row = r < left ? r : (uint32_t)(left - 1);
         at[i] = row * (uint32_t)p.pitch + ((((uint32_t)lane & 7) ^ ((r >> 1) & 7)) << 4);
     }
-    // and 64 rows' scales, one of (TA + TB) / 64 pieces (in tiles of fewer rows than lanes several wavefronts load the same piece)
-    constexpr int kScalePieces = (TA + TB) / 64;
-    static_assert(TA % 64 == 0 && TB % 64 == 0 && kScalePieces <= kWaves);
-    const int piece = wave % kScalePieces, piece_op = 64 * piece >= TA, piece_r = 64 * piece + lane - (piece_op ? TA : 0);
-    const int64_t piece_row0 = piece_op ? t0 : m0, piece_left = (piece_op ? p.T : p.M) - piece_row0;
-    const int64_t piece_row = piece_r < piece_left ? piece_r : piece_left - 1;
-    const bool blocks = !piece_op && p.block;
-    const uint8_t *scale_base = piece_op ? p.SA + t0 * p.steps : p.SB + (blocks ? m0 / 128 : m0) * p.steps;
-    const uint32_t scale_at = (uint32_t)(blocks ? (m0 + piece_row) / 128 - m0 / 128 : piece_row) * (uint32_t)p.steps;
+    // and 64 rows' scales to a piece (in tiles of fewer pieces than wavefronts several load the same one)
+    constexpr int kScalePieces = (TA + TB) / 64, kScaleLoads = (kScalePieces + kWaves - 1) / kWaves;
+    static_assert(TA % 64 == 0 && TB % 64 == 0 && (kScalePieces % kWaves == 0 || kScalePieces < kWaves));
+    const uint8_t *scale_base[kScaleLoads];
+    uint32_t scale_at[kScaleLoads], scale_lds[kScaleLoads];
+#pragma unroll
+    for (int i = 0; i < kScaleLoads; ++i) {
+        const int piece = (wave * kScaleLoads + i) % kScalePieces, op = 64 * piece >= TA, r = 64 * piece + lane - (op ? TA : 0);
+        const int64_t row0 = op ? t0 : m0, left = (op ? p.T : p.M) - row0, row = r < left ? r : left - 1;
+        const bool blocks = !op && p.block;
+        scale_base[i] = op ? p.SA + t0 * p.steps : p.SB + (blocks ? m0 / 128 : m0) * p.steps;
+        scale_at[i] = (uint32_t)(blocks ? (m0 + row) / 128 - m0 / 128 : row) * (uint32_t)p.steps;
+        scale_lds[i] = (uint32_t)(kCodes + piece * 256);
+    }
     auto load = [&](int step, int slot) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int r8 = wave * kLoads + i, op = 8 * r8 >= TA;
             load_to_lds(slot * kStage + r8 * 1024, base[op] + (int64_t)step * 128, at[i]);
         }
-        load_bytes_to_lds(slot * kStage + kCodes + piece * 256, scale_base + step, scale_at);
+#pragma unroll
+        for (int i = 0; i < kScaleLoads; ++i) load_bytes_to_lds(slot * kStage + scale_lds[i], scale_base[i] + step, scale_at[i]);
     };
     f32x16 acc[FA][FB];
 #pragma unroll
@@ -116,6 +122,10 @@ __global__ __launch_bounds__(64 * WA * WB) void fp8_tile_kernel(Product p) {
         return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
     };
 
+    // the bias of the tile's outputs, one per thread, asked for before the operands
+    static_assert(TA <= kThreads);
+    float own_bias = 0.0f;
+    if (p.bias && !p.partial && tid < TA) own_bias = elem<DT>::load(p.bias, m0 + tid < p.M ? m0 + tid : p.M - 1);
     static_for<0, NS - 1>([&](auto n) {
         if (first + n < last) load(first + n, n);  // uniform
     });
@@ -123,7 +133,7 @@ __global__ __launch_bounds__(64 * WA * WB) void fp8_tile_kernel(Product p) {
     int slot = 0;
     for (int s = first; s < last; ++s) {
         // this step's loads are done where no more are left than those of the NS - 2 steps behind it; at the end there are fewer
-        if (NS > 2 && s + NS - 1 < last + 1) wait_loads<(NS - 2) * (kLoads + 1)>();
+        if (NS > 2 && s + NS - 1 < last + 1) wait_loads<(NS - 2) * (kLoads + kScaleLoads)>();
         else wait_loads<0>();
         barrier();  // this step is in LDS, and nobody reads the slot before it any more
         if (s + NS - 1 < last) load(s + NS - 1, slot == 0 ? NS - 1 : slot - 1);
@@ -162,16 +172,64 @@ __global__ __launch_bounds__(64 * WA * WB) void fp8_tile_kernel(Product p) {
         slot = slot == NS - 1 ? 0 : slot + 1;
     }
 
-    // A pass of 32 WB tokens: sums to LDS, then whole rows leave with bias, activation and residual
+    // 16-bit results without a residual: finished where they are, rounded into a tile of all tokens in LDS, and out in whole rows.
+    if constexpr (DT != BSP_F32) {
+        constexpr int kRow = TA * 2 + 16;
+        static_assert(TB * kRow <= NS * kStage);
+        if (!p.partial && !p.residual) {
+            float *biases = reinterpret_cast<float *>(smem + NS * kStage);
+            if (tid < TA) biases[tid] = own_bias;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < FA; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int c = (wa * FA + i) * 32 + 8 * q + 4 * half;
+                    const f32x4 b = *reinterpret_cast<const f32x4 *>(biases + c);
+#pragma unroll
+                    for (int j = 0; j < FB; ++j) {
+                        float v[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            v[k] = acc[i][j][4 * q + k] + b[k];
+                            if (p.act == BSP_ACT_GELU) v[k] = gelu_fit(v[k]);
+                        }
+                        *reinterpret_cast<uint2 *>(smem + ((wb * FB + j) * 32 + l32) * kRow + c * 2) = make_uint2(cvt_pk<DT>(v[0], v[1]), cvt_pk<DT>(v[2], v[3]));
+                    }
+                }
+            __syncthreads();
+            const int cols = p.M - m0 < TA ? (int)(p.M - m0) : TA, rows = p.T - t0 < TB ? (int)(p.T - t0) : TB;
+            uint16_t *y = (uint16_t *)p.Y + t0 * p.M + m0;
+            const bool vec = (p.M & 7) == 0 && (reinterpret_cast<uintptr_t>(p.Y) & 15) == 0;
+            for (int n = tid; n < TB * (TA / 8); n += kThreads) {
+                const int r = n / (TA / 8), c = n % (TA / 8) * 8;
+                if (r >= rows || c >= cols) continue;
+                const uint4 x = *reinterpret_cast<const uint4 *>(smem + r * kRow + c * 2);
+                uint16_t *o = y + (int64_t)r * p.M + c;
+                if (vec) {
+                    store_y16(o, x);
+                } else if (c + 8 <= cols) {
+                    __builtin_memcpy(o, &x, 16);  // (stores need no alignment either)
+                } else {
+                    for (int k = 0; k < cols - c; ++k) o[k] = *reinterpret_cast<const uint16_t *>(smem + r * kRow + (c + k) * 2);
+                }
+            }
+            return;
+        }
+    }
+    // Else a pass of 32 WB tokens: sums to LDS, then whole rows leave with bias, activation and residual
     float *out = reinterpret_cast<float *>(smem);
     const bool vec = (p.M & 7) == 0;
     constexpr int kPiece = TA / 8;  // threads of a row
     const int c = (tid % kPiece) * 8;
     const int64_t m = m0 + c;
     const int cols = p.M - m > 8 ? 8 : (int)(p.M - m);
+    float *biases = reinterpret_cast<float *>(smem + (NS * kStage > 32 * WB * kPitch * 4 ? NS * kStage : 32 * WB * kPitch * 4));
+    if (tid < TA) biases[tid] = own_bias;
+    __syncthreads();
     float bias[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) bias[k] = p.bias && !p.partial && k < cols ? elem<DT>::load(p.bias, m + k) : 0.0f;
+    for (int k = 0; k < 8; ++k) bias[k] = biases[c + k];
 #pragma unroll
     for (int j = 0; j < FB; ++j) {
         __syncthreads();
@@ -208,8 +266,8 @@ __global__ __launch_bounds__(64 * WA * WB) void fp8_tile_kernel(Product p) {
 // Up to 16 NT tokens: B is read once and straight into registers (a wavefront's 16 rows x 128 columns are whole lines), the steps of 128
 // columns dealt to the workgroup's wavefronts in turn, whose sums meet in LDS in ascending order.  What bounds it is B's way from memory,
 // and for small matrices the launch.
-// RAW: the tokens come in XDT and are quantised here, in registers, by every workgroup for itself: 32 values of a lane, four lanes to
-// a segment.  That is less than a launch of its own for one tile of tokens.
+// RAW: the tokens come as they are and are quantised here, in registers, by every workgroup for itself: 32 values of a lane, four lanes to
+// a segment.  That is less than a launch of its own.
 constexpr int kFewWaves = 8;
 
 template <int XDT>
@@ -330,39 +388,59 @@ __global__ __launch_bounds__(256) void fp8_join_kernel(Product p, int splits) {
     finish8<DT>(v, bias, p.act, p.residual, p.Y, (int64_t)t * p.M + m, (p.M & 7) == 0, cols);
 }
 
-constexpr int64_t kFewTokens = 64;  // of fp8_few_kernel
-constexpr int64_t kRawTokens = 16;  // quantised by every workgroup
+constexpr int64_t kFewTokens = 32;  // of fp8_few_kernel
+
+// Whether its workgroups quantise the tokens themselves: where a wavefront has one step of it to do, or two for one tile of tokens.  (us, in
+// one launch / in two: 1 token of 1024 columns, 4096 rows 4.1 / 5.3; 32 tokens 6.0 / 6.4; 1 token of 4096 columns 10.5 / 8.1, 32 tokens 18.4 / 12.8.)
+bool quantised_inside(int64_t T, int64_t steps) { return T <= 16 ? steps <= 2 * kFewWaves : T <= kFewTokens && steps <= kFewWaves; }
 
 struct Shape {
-    int tile;    // 256, 128 or 64; 0: few tokens
+    int tile;    // 256, 128, 64, or 63: 64 with its steps four deep in LDS; 0: few tokens
     int splits, split_steps;
 };
 
-Shape choose(int64_t T, int64_t M, int64_t steps) {
-    Shape s = {256, 1, (int)steps};
-    if (T <= kFewTokens) {
-        s.tile = 0;
-        return s;
+// Microseconds of a product in tiles of `tile` x `tile`, `n` of them (with the splits), of `steps` steps; fitted to 60 shapes of 32 to 16384 rows
+// and 1024 to 16384 columns.  `wide`: fp32 results, whose instructions take twice as long.  A larger tile loads less for a product, but its
+// workgroups leave compute units idle at the end of a round, and one of 256 x 256 fills a compute unit, so that its epilogue (GELU: 6 us a round)
+// hides nothing.  Measured, 256 / 128 / 64 / 63: 16384 x 4096, K = 4096 234 / 268 / 418 / 463; 8192 x 4096, K = 1024 43 / 45 / 62 / 77, with GELU
+// 57 / 53 / 68; 8192 x 1024, K = 4096 50 / 37 / 59 / 62; 1024 x 1024, K = 1024 19 / 9.1 / 7.8 / 7.9; 512 x 1024, K = 4096 53 / 27 / 20 / 12.5.
+double tile_us(int tile, double n, double steps, bool wide, bool gelu) {
+    const double rounds256 = __builtin_ceil(n / 256.0);
+    if (tile == 256) return 5.0 + rounds256 * ((wide ? 3.2 : 1.62) * steps + 5.0 + (gelu ? 6.0 : 0.0));
+    if (tile == 128) {
+        if (n <= 256.0) return 5.0 + (wide ? 1.12 : 0.72) * steps + (gelu ? 2.5 : 0.0);
+        return 3.5 + __builtin_ceil(n / 512.0) * ((wide ? 1.85 : 1.03) * steps + 2.2 + (gelu ? 2.5 : 0.0));
     }
-    auto count = [&](int64_t t) { return ((T + t - 1) / t) * ((M + t - 1) / t); };
-    if (count(256) < 192) s.tile = 128;
-    if (s.tile == 128 && count(128) < 192) s.tile = 64;
-    const int64_t n = count(s.tile);
-    if (n < 128 && steps >= 8) {
-        int64_t k = 256 / n;
-        if (k > steps / 4) k = steps / 4;
-        if (k > 1) {
-            s.split_steps = (int)((steps + k - 1) / k);
-            s.splits = (int)((steps + s.split_steps - 1) / s.split_steps);
+    if (tile == 64) return 3.5 + __builtin_ceil(n / 1024.0) * ((wide ? 1.25 : 0.83) * steps + 1.6 + (gelu ? 1.0 : 0.0));
+    if (n <= 256.0) return 5.5 + (wide ? 0.48 : 0.23) * steps;
+    return 3.5 + __builtin_ceil(n / 512.0) * ((wide ? 0.8 : 0.44) * steps + 2.2 + (gelu ? 0.5 : 0.0));
+}
+
+// The tile, and into how many runs the steps are split where there are too few tiles for the compute units (256 x 256, K = 16384 in fp32: 60 us,
+// 15.7 in eight runs; 1024 x 1024, K = 8192 34.9 and 30.5 in two).  A split costs a launch and its sums' way to memory and back.
+Shape choose(int64_t T, int64_t M, int64_t steps, bool wide, bool gelu) {
+    Shape best = {0, 1, (int)steps};
+    if (T <= kFewTokens) return best;
+    double least = 0.0;
+    for (int tile : {256, 128, 64, 63}) {
+        const double side = tile == 63 ? 64.0 : (double)tile, n = __builtin_ceil((double)T / side) * __builtin_ceil((double)M / side);
+        for (int k = 1; k <= 16; k *= 2) {
+            if (k > 1 && (steps < 4 * k || n * k > 512.0)) break;
+            const int64_t each = (steps + k - 1) / k;
+            double us = tile_us(tile, n * k, (double)each, wide, gelu);
+            if (k > 1) us += 4.5 + (double)T * (double)M * (8.0 * k + 4.0) / 5e6;
+            if (least != 0.0 && us >= least) continue;
+            least = us;
+            best = {tile, (int)((steps + each - 1) / each), (int)each};
         }
     }
-    return s;
+    return best;
 }
 
 template <int DT, int FA, int FB, int WA, int WB, int NS>
 int launch_tile(const Product &p, int splits, hipStream_t s) {
     constexpr int TA = 32 * FA * WA, TB = 32 * FB * WB;
-    constexpr size_t stages = NS * (size_t)(TA + TB) * 132, out = (size_t)32 * WB * (TA + 4) * 4, lds = stages > out ? stages : out;
+    constexpr size_t stages = NS * (size_t)(TA + TB) * 132, out = (size_t)32 * WB * (TA + 4) * 4, lds = (stages > out ? stages : out) + TA * 4;
     auto k = fp8_tile_kernel<DT, FA, FB, WA, WB, NS>;
     if (lds > 65536) {  // (asking again is harmless)
         hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -380,13 +458,8 @@ int launch_tile(const Product &p, int splits, hipStream_t s) {
 template <int DT, bool RAW>
 int launch_few(const Product &p, const void *X, int64_t N, hipStream_t s) {
     const unsigned grid = (unsigned)((p.M + 15) / 16), threads = 64u * (unsigned)(p.steps < kFewWaves ? p.steps : kFewWaves);
-    if constexpr (RAW) {
-        fp8_few_kernel<DT, 1, true><<<grid, threads, 0, s>>>(p, X, N);
-    } else {
-        if (p.T <= 16) fp8_few_kernel<DT, 1, false><<<grid, threads, 0, s>>>(p, X, N);
-        else if (p.T <= 32) fp8_few_kernel<DT, 2, false><<<grid, threads, 0, s>>>(p, X, N);
-        else fp8_few_kernel<DT, 4, false><<<grid, threads, 0, s>>>(p, X, N);
-    }
+    if (p.T <= 16) fp8_few_kernel<DT, 1, RAW><<<grid, threads, 0, s>>>(p, X, N);
+    else fp8_few_kernel<DT, 2, RAW><<<grid, threads, 0, s>>>(p, X, N);
     return check_launch();
 }
 
@@ -395,7 +468,8 @@ int launch_product(const Product &p, const Shape &c, hipStream_t s) {
     int st;
     if (c.tile == 0) return launch_few<DT, false>(p, nullptr, 0, s);
     if (c.tile == 256) st = launch_tile<DT, 2, 4, 4, 2, 2>(p, c.splits, s);
-    else if (c.tile == 128) st = launch_tile<DT, 2, 2, 2, 2, 2>(p, c.splits, s);
+    else if (c.tile == 128) st = launch_tile<DT, 2, 1, 2, 4, 2>(p, c.splits, s);
+    else if (c.tile == 64) st = launch_tile<DT, 1, 1, 2, 2, 2>(p, c.splits, s);
     else st = launch_tile<DT, 1, 1, 2, 2, 4>(p, c.splits, s);
     if (st || c.splits == 1) return st;
     const int64_t n = p.T * ((p.M + 7) / 8);
@@ -410,9 +484,15 @@ size_t partial_bytes(const Shape &c, int64_t T, int64_t M) {
     return c.splits > 1 ? (size_t)c.splits * (size_t)T * (size_t)((M + 7) / 8 * 8) * 4 : 0;
 }
 
+// (for either kind of result: the query does not know it)
 size_t split_bytes(int64_t T, int64_t M, int64_t K) {
-    const Shape c = choose(T, M, steps_of(K));
-    return partial_bytes(c, T, M);
+    size_t most = 0;
+    for (bool wide : {false, true})
+        for (bool gelu : {false, true}) {
+            const size_t n = partial_bytes(choose(T, M, steps_of(K), wide, gelu), T, M);
+            most = n > most ? n : most;
+        }
+    return most;
 }
 
 int check_sizes(int64_t T, int64_t M, int64_t K, int layout, int ydt, int act) {
@@ -423,7 +503,7 @@ int check_sizes(int64_t T, int64_t M, int64_t K, int layout, int ydt, int act) {
 
 int product(const void *A, const uint8_t *SA, const void *B, const uint8_t *SB, int layout, int64_t T, int64_t M, int64_t K, const void *bias,
             int act, const void *residual, void *Y, int ydt, void *ws, size_t ws_bytes, hipStream_t s) {
-    Shape c = choose(T, M, steps_of(K));
+    Shape c = choose(T, M, steps_of(K), ydt == BSP_F32, act == BSP_ACT_GELU);
     if (ws_bytes < partial_bytes(c, T, M)) c.splits = 1, c.split_steps = (int)steps_of(K);
     const Product p = {(const uint8_t *)A, SA, (const uint8_t *)B, SB, bias, residual, Y, c.splits > 1 ? (float *)ws : nullptr, T, M,
                        (int32_t)steps_of(K), (int32_t)(128 * steps_of(K)), c.split_steps, layout == BSP_FP8_BLOCK, act};
@@ -457,7 +537,7 @@ extern "C" int bsp_matmul_fp8(const void *A, const uint8_t *SA, const void *B, c
 
 extern "C" size_t bsp_linear_fp8_workspace_bytes(int64_t T, int64_t M, int64_t N) {
     if (T <= 0 || check_sizes(T, M, N, BSP_FP8_ROW, BSP_F32, BSP_ACT_NONE)) return 0;
-    if (T <= kRawTokens) return 0;
+    if (quantised_inside(T, steps_of(N))) return 0;
     return up256((size_t)T * 128 * steps_of(N)) + up256((size_t)T * steps_of(N)) + split_bytes(T, M, N);
 }
 
@@ -465,7 +545,7 @@ extern "C" int bsp_linear_fp8(const void *X, int xdt, int64_t T, int64_t M, int6
                               const void *bias, int act, const void *residual, void *Y, void *ws, size_t ws_bytes, void *stream) {
     if (int st = check_sizes(T, M, N, w_layout, xdt, act)) return st;
     if (T == 0) return BSP_OK;
-    const bool raw = T <= kRawTokens;
+    const bool raw = quantised_inside(T, steps_of(N));
     if (!X || !W || !SW || !Y || (!raw && !ws)) return BSP_ERR_NULL;
     const size_t size = dtype_size(xdt);
     if (!aligned(X, size) || !aligned(W, 16) || !aligned(Y, size) || !aligned(bias, size) || !aligned(residual, size) || !aligned(ws, 256)) return BSP_ERR_SHAPE;
