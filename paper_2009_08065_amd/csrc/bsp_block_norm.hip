@@ -11,70 +11,97 @@
 // sum of squares less the square of the sum would lose where the mean is large.  The sums down the columns (gradients of w, b and gate) are kept
 // in registers over the rows of a workgroup, and a second launch adds the workgroups' sums in ascending order: equal calls give equal bits.
 #include "bsp_common.h"
+#include "bsp_mfma_device.h"
 
 namespace bsp {
 namespace {
 
 constexpr int kMaxH = 8192;
-constexpr int kVec = 8;  // values of a piece: consecutive ones of a thread (VEC), or one per thread and step (any alignment)
+constexpr int kVec = 8;  // values of a piece
 
-// Piece u of a thread's share of a row: columns of its value j.
-template <int TPR, bool VEC>
+// Column of value j of piece u of thread t's share of a row.  WHOLE: a piece is 8 neighbouring columns, 16 or 32 bytes in one go (at any address: loads
+// and stores need no alignment).  Where the width is no multiple of 8 a piece is 8 columns a team's width apart (1536 x 770 in fp32, backward:
+// 22 us, 32 with whole pieces and one that ends inside).
+template <int TPR, bool WHOLE>
 __device__ __forceinline__ int column(int u, int j, int t) {
-    return VEC ? (u * TPR + t) * kVec + j : (u * kVec + j) * TPR + t;
+    return WHOLE ? (u * TPR + t) * kVec + j : (u * kVec + j) * TPR + t;
 }
 
-template <int DT, int TPR, bool VEC>
-__device__ __forceinline__ void load_piece(float (&v)[kVec], const void *p, int64_t at, int u, int t, int H) {
-    if constexpr (VEC) {
-        const int c = column<TPR, true>(u, 0, t);
-        if (c < H) {
-            if constexpr (DT == BSP_F32) {
-                const float4 a = *reinterpret_cast<const float4 *>((const float *)p + at + c);
-                const float4 b = *reinterpret_cast<const float4 *>((const float *)p + at + c + 4);
-                v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+// The row of H elements at element `at`, as a buffer: past its end loads give 0 and stores write nothing.  (A team's row is the same for all
+// lanes of a wavefront.  With a comparison and a branch for every element the kernel's code, which a short call runs through once, took
+// most of its time.)
+template <int SIZE>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of_row(const void *p, int64_t at, int H) {
+    const uint64_t a = (uint64_t)p + at * SIZE;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a), hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
+    return __builtin_amdgcn_make_buffer_rsrc((void *)((uint64_t)hi << 32 | lo), 0, H * SIZE, 0x00020000);
+}
+
+// A piece as it lies in memory.
+template <int DT, int TPR, bool WHOLE>
+struct Raw {
+    uint4 d[DT == BSP_F32 ? 2 : 1];
+    // of the row of H columns at element `at`
+    __device__ __forceinline__ void load(const void *p, int64_t at, int u, int t, int H) {
+        constexpr int size = DT == BSP_F32 ? 4 : 2;
+        if constexpr (WHOLE) {
+            const int c = column<TPR, true>(u, 0, t);
+            if (c < H) {
+                __builtin_memcpy(d, (const uint8_t *)p + (at + c) * size, sizeof(d));
             } else {
-                const uint4 a = *reinterpret_cast<const uint4 *>((const uint16_t *)p + at + c);
-                const uint32_t d[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint16_t lo = (uint16_t)d[j], hi = (uint16_t)(d[j] >> 16);
-                    v[2 * j] = elem<DT>::load(&lo, 0);
-                    v[2 * j + 1] = elem<DT>::load(&hi, 0);
-                }
+                for (uint4 &x : d) x = make_uint4(0u, 0u, 0u, 0u);
             }
         } else {
+            const __amdgpu_buffer_rsrc_t row = buffer_of_row<size>(p, at, H);
+            uint32_t w[8];
 #pragma unroll
-            for (int j = 0; j < kVec; ++j) v[j] = 0.0f;
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < kVec; ++j) {
-            const int c = column<TPR, false>(u, j, t);
-            v[j] = c < H ? elem<DT>::load(p, at + c) : 0.0f;
+            for (int j = 0; j < kVec; ++j) {
+                const int c = size * column<TPR, false>(u, j, t);
+                if constexpr (DT == BSP_F32) w[j] = __builtin_amdgcn_raw_buffer_load_b32(row, c, 0, 0);
+                else w[j] = __builtin_amdgcn_raw_buffer_load_b16(row, c, 0, 0);
+            }
+            if constexpr (DT == BSP_F32) {
+                d[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                d[1] = make_uint4(w[4], w[5], w[6], w[7]);
+            } else {
+                d[0] = make_uint4(w[0] | (w[1] << 16), w[2] | (w[3] << 16), w[4] | (w[5] << 16), w[6] | (w[7] << 16));
+            }
         }
     }
-}
+    __device__ __forceinline__ float operator[](int j) const {
+        if constexpr (DT == BSP_F32) {
+            const uint32_t w[8] = {d[0].x, d[0].y, d[0].z, d[0].w, d[1].x, d[1].y, d[1].z, d[1].w};
+            return __uint_as_float(w[j]);
+        } else {
+            const uint32_t w[4] = {d[0].x, d[0].y, d[0].z, d[0].w};
+            const uint16_t h = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+            return elem<DT>::load(&h, 0);
+        }
+    }
+};
 
-template <int DT, int TPR, bool VEC>
+template <int DT, int TPR, bool WHOLE>
 __device__ __forceinline__ void store_piece(const float (&v)[kVec], void *p, int64_t at, int u, int t, int H) {
-    if constexpr (VEC) {
+    if constexpr (WHOLE) {
         const int c = column<TPR, true>(u, 0, t);
         if (c >= H) return;
         if constexpr (DT == BSP_F32) {
-            *reinterpret_cast<float4 *>((float *)p + at + c) = make_float4(v[0], v[1], v[2], v[3]);
-            *reinterpret_cast<float4 *>((float *)p + at + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
+            __builtin_memcpy((float *)p + at + c, v, 32);
         } else {
             uint32_t d[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) d[j] = elem<DT>::bits(v[2 * j]) | (elem<DT>::bits(v[2 * j + 1]) << 16);
-            *reinterpret_cast<uint4 *>((uint16_t *)p + at + c) = make_uint4(d[0], d[1], d[2], d[3]);
+            for (int j = 0; j < 4; ++j) d[j] = cvt_pk<DT>(v[2 * j], v[2 * j + 1]);
+            __builtin_memcpy((uint16_t *)p + at + c, d, 16);
         }
     } else {
+        constexpr int size = DT == BSP_F32 ? 4 : 2;
+        const __amdgpu_buffer_rsrc_t row = buffer_of_row<size>(p, at, H);
 #pragma unroll
         for (int j = 0; j < kVec; ++j) {
-            const int c = column<TPR, false>(u, j, t);
-            if (c < H) elem<DT>::store(p, at + c, v[j]);
+            const int c = size * column<TPR, false>(u, j, t);
+            if constexpr (DT == BSP_F32) __builtin_amdgcn_raw_buffer_store_b32(elem<DT>::bits(v[j]), row, c, 0, 0);
+            else __builtin_amdgcn_raw_buffer_store_b16((uint16_t)elem<DT>::bits(v[j]), row, c, 0, 0);
         }
     }
 }
@@ -88,17 +115,31 @@ __device__ __forceinline__ float rounded(float v) {
     }
 }
 
-// Sums of K values over the TPR threads of a team, in every one of them.  LDS: `red` of K * TPR / 64 floats, two of them in turn, so that
+// The sum of 64 lanes' values, in every lane: within rows of 16 lanes and then across them (an exchange through LDS takes ten times as long, and
+// a row waits for up to four of these in turn).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float add_dpp(float x) {
+    return x + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float wave_sum(float x) {
+    x = add_dpp<0x111, 0xf>(x);  // row_shr 1, 2, 4, 8: lane 15 of a row has the row's
+    x = add_dpp<0x112, 0xf>(x);
+    x = add_dpp<0x114, 0xf>(x);
+    x = add_dpp<0x118, 0xf>(x);
+    x = add_dpp<0x142, 0xa>(x);  // row_bcast 15 into rows 1 and 3, 31 into rows 2 and 3
+    x = add_dpp<0x143, 0xc>(x);
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), 63));
+}
+
+// Sums of K values over the TPR threads of a team, in every one of them.  LDS: `red` of 2 * K * TPR / 64 floats, its halves in turn, so that
 // one barrier a sum is enough.
 template <int TPR, int K>
 __device__ __forceinline__ void team_sum(float (&v)[K], float *red, int &turn) {
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1)
-#pragma unroll
-        for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], d);
+    for (int k = 0; k < K; ++k) v[k] = wave_sum(v[k]);
     if constexpr (TPR > 64) {
         constexpr int W = TPR / 64;
-        float *r = red + turn * 2 * W;
+        float *r = red + turn * K * W;
         turn ^= 1;
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
@@ -124,7 +165,7 @@ struct Forward {
 };
 
 // One team's row: mean and 1 / deviation of the values v (columns past the width hold 0 and are not part of it).
-template <int TPR, int ITER, bool VEC>
+template <int TPR, int ITER, bool WHOLE>
 __device__ __forceinline__ void statistics(const float (&v)[ITER][kVec], int t, const Forward &a, float &mean, float &rstd, float *red, int &turn) {
     mean = 0.0f;
     const float n = 1.0f / (float)a.width;
@@ -143,82 +184,78 @@ __device__ __forceinline__ void statistics(const float (&v)[ITER][kVec], int t, 
 #pragma unroll
         for (int j = 0; j < kVec; ++j) {
             const float d = v[u][j] - mean;
-            q[0] = column<TPR, VEC>(u, j, t) < a.width ? __builtin_fmaf(d, d, q[0]) : q[0];
+            q[0] = column<TPR, WHOLE>(u, j, t) < a.width ? __builtin_fmaf(d, d, q[0]) : q[0];
         }
     team_sum<TPR, 1>(q, red, turn);
     rstd = 1.0f / __builtin_sqrtf(q[0] * n + a.eps);
 }
 
-template <int DT, int TPR, int ITER, bool VEC>
-__device__ __forceinline__ void normalise(float (&v)[ITER][kVec], float mean, float rstd, const void *w, const void *b, int t, int H) {
-#pragma unroll
-    for (int u = 0; u < ITER; ++u) {
-        float x[kVec];
-#pragma unroll
-        for (int j = 0; j < kVec; ++j) v[u][j] = (v[u][j] - mean) * rstd;
-        if (w) {
-            load_piece<DT, TPR, VEC>(x, w, 0, u, t, H);
-#pragma unroll
-            for (int j = 0; j < kVec; ++j) v[u][j] *= x[j];
-        }
-        if (b) {
-            load_piece<DT, TPR, VEC>(x, b, 0, u, t, H);
-#pragma unroll
-            for (int j = 0; j < kVec; ++j) v[u][j] += x[j];
-        }
-    }
-}
-
-template <int DT, int TPR, int ITER, bool VEC>
+template <int DT, int TPR, int ITER, bool WHOLE>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void block_norm_kernel(Forward a) {
     constexpr int kTeams = TPR < 256 ? 256 / TPR : 1;
-    __shared__ float red[TPR > 64 ? 4 * (TPR / 64) : 1];
+    __shared__ float red[TPR > 64 ? 2 * (TPR / 64) : 1];
     int turn = 0;
     const int t = threadIdx.x % TPR, H = a.width;
     const int64_t row = (int64_t)blockIdx.x * kTeams + threadIdx.x / TPR;
     if (row >= a.T) return;  // (whole teams; a workgroup of one team has a row)
     const int64_t at = row * H;
-    float x[ITER][kVec], f[ITER][kVec];
+    const bool post = a.F && (a.norms & BSP_NORM_POST), pre = (a.norms & BSP_NORM_PRE) != 0;
+    // everything is asked for before the first sum is waited for
+    using Piece = Raw<DT, TPR, WHOLE>;
+    Piece rx[ITER], rf[ITER], rg[ITER], w1[ITER], b1[ITER], w2[ITER], b2[ITER];
+    auto ask = [&](Piece(&r)[ITER], const void *p, int64_t from) {
+        if (p)
 #pragma unroll
-    for (int u = 0; u < ITER; ++u) load_piece<DT, TPR, VEC>(x[u], a.X, at, u, t, H);
+            for (int u = 0; u < ITER; ++u) r[u].load(p, from, u, t, H);
+    };
+    ask(rx, a.X, at);
+    ask(rf, a.F, at);
+    ask(w1, a.w_post, 0);
+    ask(b1, a.b_post, 0);
+    if (a.gate) ask(rg, a.gate, row / a.rows_per_gate * H);
+    ask(w2, a.w_pre, 0);
+    ask(b2, a.b_pre, 0);
+    auto normalise = [&](float(&v)[ITER][kVec], float mean, float rstd, const void *w, const Piece(&rw)[ITER], const void *b, const Piece(&rb)[ITER]) {
+#pragma unroll
+        for (int u = 0; u < ITER; ++u)
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) {
+                v[u][j] = (v[u][j] - mean) * rstd;
+                if (w) v[u][j] *= rw[u][j];
+                if (b) v[u][j] += rb[u][j];
+            }
+    };
+    float x[ITER][kVec], f[ITER][kVec];
     if (a.F) {
 #pragma unroll
-        for (int u = 0; u < ITER; ++u) load_piece<DT, TPR, VEC>(f[u], a.F, at, u, t, H);
-        if (a.norms & BSP_NORM_POST) {
+        for (int u = 0; u < ITER; ++u)
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) f[u][j] = rf[u][j];
+        if (post) {
             float mean, rstd;
-            statistics<TPR, ITER, VEC>(f, t, a, mean, rstd, red, turn);
+            statistics<TPR, ITER, WHOLE>(f, t, a, mean, rstd, red, turn);
             if (a.stats_post && t == 0) *reinterpret_cast<float2 *>(a.stats_post + 2 * row) = make_float2(mean, rstd);
-            normalise<DT, TPR, ITER, VEC>(f, mean, rstd, a.w_post, a.b_post, t, H);
-        }
-        if (a.gate) {
-            const int64_t g = row / a.rows_per_gate * H;
-#pragma unroll
-            for (int u = 0; u < ITER; ++u) {
-                float y[kVec];
-                load_piece<DT, TPR, VEC>(y, a.gate, g, u, t, H);
-#pragma unroll
-                for (int j = 0; j < kVec; ++j) f[u][j] *= y[j];
-            }
+            normalise(f, mean, rstd, a.w_post, w1, a.b_post, b1);
         }
     }
 #pragma unroll
     for (int u = 0; u < ITER; ++u)
 #pragma unroll
         for (int j = 0; j < kVec; ++j) {
-            float z = a.x_scale * x[u][j];
-            if (a.F) z += f[u][j];
-            x[u][j] = column<TPR, VEC>(u, j, t) < H ? rounded<DT>(z) : 0.0f;
+            float z = a.x_scale * rx[u][j];
+            if (a.F) z += a.gate ? f[u][j] * rg[u][j] : f[u][j];
+            x[u][j] = column<TPR, WHOLE>(u, j, t) < H ? rounded<DT>(z) : 0.0f;
         }
     if (a.Z)
 #pragma unroll
-        for (int u = 0; u < ITER; ++u) store_piece<DT, TPR, VEC>(x[u], a.Z, at, u, t, H);
-    if (a.norms & BSP_NORM_PRE) {
+        for (int u = 0; u < ITER; ++u) store_piece<DT, TPR, WHOLE>(x[u], a.Z, at, u, t, H);
+    if (pre) {
         float mean, rstd;
-        statistics<TPR, ITER, VEC>(x, t, a, mean, rstd, red, turn);
+        statistics<TPR, ITER, WHOLE>(x, t, a, mean, rstd, red, turn);
         if (a.stats_pre && t == 0) *reinterpret_cast<float2 *>(a.stats_pre + 2 * row) = make_float2(mean, rstd);
-        normalise<DT, TPR, ITER, VEC>(x, mean, rstd, a.w_pre, a.b_pre, t, H);
+        normalise(x, mean, rstd, a.w_pre, w2, a.b_pre, b2);
 #pragma unroll
-        for (int u = 0; u < ITER; ++u) store_piece<DT, TPR, VEC>(x[u], a.H, at, u, t, H);
+        for (int u = 0; u < ITER; ++u) store_piece<DT, TPR, WHOLE>(x[u], a.H, at, u, t, H);
     }
 }
 
@@ -239,13 +276,18 @@ struct Backward {
     uint32_t want;                                      // bit i: sums of kind i
 };
 
-template <int DT, int TPR, int ITER, bool VEC>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void block_norm_back_kernel(Backward a) {
-    constexpr int kTeams = TPR < 256 ? 256 / TPR : 1;
-    __shared__ float red[TPR > 64 ? 8 * (TPR / 64) : 1];
+constexpr int kBackTeams = 4;  // wavefronts of a workgroup where a row is one's (their sums meet before they leave it)
+
+// SIMPLE: BERT's form, N_pre without a gate (no F, and two sums).
+template <int DT, int TPR, int ITER, bool WHOLE, bool SIMPLE>
+__global__ __launch_bounds__(TPR == 64 ? 64 * kBackTeams : TPR) void block_norm_back_kernel(Backward a) {
+    constexpr int kTeams = TPR == 64 ? kBackTeams : 1;
+    __shared__ float red[TPR > 64 ? 4 * (TPR / 64) : 1];
     __shared__ float share[kTeams > 1 ? (kTeams - 1) * TPR * kVec : 1];
     int turn = 0;
     const int t = threadIdx.x % TPR, team = threadIdx.x / TPR, H = a.width;
+    const bool pre = SIMPLE || (a.norms & BSP_NORM_PRE), post = !SIMPLE && (a.norms & BSP_NORM_POST);
+    const void *F = SIMPLE ? nullptr : a.F, *gate = SIMPLE ? nullptr : a.gate;
     const float inv = 1.0f / (float)H;
     float acc[kSums][ITER][kVec];
     auto clear = [&](int i) {
@@ -256,150 +298,181 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void block_norm_back_kernel(
     };
 #pragma unroll
     for (int i = 0; i < kSums; ++i) clear(i);
+    using Piece = Raw<DT, TPR, WHOLE>;
+    Piece w2[ITER];
+    if (pre && a.w_pre)
+#pragma unroll
+        for (int u = 0; u < ITER; ++u) w2[u].load(a.w_pre, 0, u, t, H);
 
-    auto one_row = [&](int64_t row, int64_t group) {
+    struct Row {
+        Piece dz[ITER], dh[ITER], z[ITER], f[ITER];
+        float2 pre, post;
+    };
+    auto ask = [&](Row &r, int64_t row) {
         const int64_t at = row * H;
-        float d[ITER][kVec], x[kVec];
+        auto each = [&](Piece(&x)[ITER], const void *p) {
 #pragma unroll
-        for (int u = 0; u < ITER; ++u) {
-            if (a.dZ) load_piece<DT, TPR, VEC>(d[u], a.dZ, at, u, t, H);
-            else
-#pragma unroll
-                for (int j = 0; j < kVec; ++j) d[u][j] = 0.0f;
+            for (int u = 0; u < ITER; ++u) x[u].load(p, at, u, t, H);
+        };
+        if (a.dZ) each(r.dz, a.dZ);
+        if (pre) {
+            each(r.dh, a.dH);
+            each(r.z, a.Z);
+            r.pre = *reinterpret_cast<const float2 *>(a.stats_pre + 2 * row);
         }
-        float f[ITER][kVec];
-        if (a.F)
+        if (F) each(r.f, F);
+        if (post) r.post = *reinterpret_cast<const float2 *>(a.stats_post + 2 * row);
+    };
+    auto one_row = [&](const Row &r, int64_t row, int64_t group) {
+        const int64_t at = row * H;
+        float d[ITER][kVec];
 #pragma unroll
-            for (int u = 0; u < ITER; ++u) load_piece<DT, TPR, VEC>(f[u], a.F, at, u, t, H);
-        if (a.norms & BSP_NORM_PRE) {
-            float h[ITER][kVec], z[ITER][kVec];
-            const float2 st = *reinterpret_cast<const float2 *>(a.stats_pre + 2 * row);
+        for (int u = 0; u < ITER; ++u)
 #pragma unroll
-            for (int u = 0; u < ITER; ++u) load_piece<DT, TPR, VEC>(h[u], a.dH, at, u, t, H);
-#pragma unroll
-            for (int u = 0; u < ITER; ++u) load_piece<DT, TPR, VEC>(z[u], a.Z, at, u, t, H);
+            for (int j = 0; j < kVec; ++j) d[u][j] = a.dZ ? r.dz[u][j] : 0.0f;
+        if (pre) {
             float s[2] = {0.0f, 0.0f};
 #pragma unroll
-            for (int u = 0; u < ITER; ++u) {
-                if (a.w_pre) load_piece<DT, TPR, VEC>(x, a.w_pre, 0, u, t, H);
+            for (int u = 0; u < ITER; ++u)
 #pragma unroll
                 for (int j = 0; j < kVec; ++j) {
-                    const float hat = (z[u][j] - st.x) * st.y, dh = h[u][j];
+                    const float hat = (r.z[u][j] - r.pre.x) * r.pre.y, dh = r.dh[u][j];
                     acc[kDwPre][u][j] = __builtin_fmaf(dh, hat, acc[kDwPre][u][j]);
                     acc[kDbPre][u][j] += dh;
-                    const float g = a.w_pre ? dh * x[j] : dh;
+                    const float g = a.w_pre ? dh * w2[u][j] : dh;
                     s[0] = __builtin_fmaf(g, hat, s[0]);  // (past the width dh is 0)
                     s[1] += g;
-                    z[u][j] = hat;
-                    h[u][j] = g;
                 }
-            }
             team_sum<TPR, 2>(s, red, turn);
             const float c1 = s[0] * inv, c2 = a.rms ? 0.0f : s[1] * inv;
 #pragma unroll
             for (int u = 0; u < ITER; ++u)
 #pragma unroll
-                for (int j = 0; j < kVec; ++j) d[u][j] += st.y * (h[u][j] - z[u][j] * c1 - c2);
+                for (int j = 0; j < kVec; ++j) {
+                    const float hat = (r.z[u][j] - r.pre.x) * r.pre.y, dh = r.dh[u][j];
+                    d[u][j] += r.pre.y * ((a.w_pre ? dh * w2[u][j] : dh) - hat * c1 - c2);
+                }
         }
         if (a.dX)
 #pragma unroll
             for (int u = 0; u < ITER; ++u) {
+                float x[kVec];
 #pragma unroll
                 for (int j = 0; j < kVec; ++j) x[j] = a.x_scale * d[u][j];
-                store_piece<DT, TPR, VEC>(x, a.dX, at, u, t, H);
+                store_piece<DT, TPR, WHOLE>(x, a.dX, at, u, t, H);
             }
-        const bool post = (a.norms & BSP_NORM_POST) != 0;
-        float2 st = make_float2(0.0f, 0.0f);
-        if (post) st = *reinterpret_cast<const float2 *>(a.stats_post + 2 * row);
-        float s[2] = {0.0f, 0.0f};
+        if constexpr (!SIMPLE) {
+            float s[2] = {0.0f, 0.0f};
 #pragma unroll
-        for (int u = 0; u < ITER; ++u) {
-            float w[kVec], b[kVec];
-            if (a.gate) load_piece<DT, TPR, VEC>(x, a.gate, group * H, u, t, H);
-            if (post && a.w_post) load_piece<DT, TPR, VEC>(w, a.w_post, 0, u, t, H);
-            if (post && a.b_post) load_piece<DT, TPR, VEC>(b, a.b_post, 0, u, t, H);
+            for (int u = 0; u < ITER; ++u) {
+                Piece w, b, y;
+                if (gate) y.load(gate, group * H, u, t, H);
+                if (post && a.w_post) w.load(a.w_post, 0, u, t, H);
+                if (post && a.b_post) b.load(a.b_post, 0, u, t, H);
 #pragma unroll
-            for (int j = 0; j < kVec; ++j) {
-                if (column<TPR, VEC>(u, j, t) >= H) {
-                    d[u][j] = 0.0f;
-                    continue;
-                }
-                float n = a.F ? f[u][j] : 0.0f, hat = 0.0f;
-                if (post) {
-                    hat = (n - st.x) * st.y;
-                    n = a.w_post ? hat * w[j] : hat;
-                    if (a.b_post) n += b[j];
-                }
-                if (a.gate) {
-                    acc[kDgate][u][j] = __builtin_fmaf(d[u][j], n, acc[kDgate][u][j]);
-                    d[u][j] *= x[j];
-                }
-                if (post) {
-                    acc[kDwPost][u][j] = __builtin_fmaf(d[u][j], hat, acc[kDwPost][u][j]);
-                    acc[kDbPost][u][j] += d[u][j];
-                    if (a.w_post) d[u][j] *= w[j];
-                    s[0] = __builtin_fmaf(d[u][j], hat, s[0]);
-                    s[1] += d[u][j];
-                    f[u][j] = hat;
+                for (int j = 0; j < kVec; ++j) {
+                    if (column<TPR, WHOLE>(u, j, t) >= H) {
+                        d[u][j] = 0.0f;
+                        continue;
+                    }
+                    float n = F ? r.f[u][j] : 0.0f, hat = 0.0f;
+                    if (post) {
+                        hat = (n - r.post.x) * r.post.y;
+                        n = a.w_post ? hat * w[j] : hat;
+                        if (a.b_post) n += b[j];
+                    }
+                    if (gate) {
+                        acc[kDgate][u][j] = __builtin_fmaf(d[u][j], n, acc[kDgate][u][j]);
+                        d[u][j] *= y[j];
+                    }
+                    if (post) {
+                        acc[kDwPost][u][j] = __builtin_fmaf(d[u][j], hat, acc[kDwPost][u][j]);
+                        acc[kDbPost][u][j] += d[u][j];
+                        if (a.w_post) d[u][j] *= w[j];
+                        s[0] = __builtin_fmaf(d[u][j], hat, s[0]);
+                        s[1] += d[u][j];
+                    }
                 }
             }
-        }
-        if (post) {
-            team_sum<TPR, 2>(s, red, turn);
-            const float c1 = s[0] * inv, c2 = a.rms ? 0.0f : s[1] * inv;
+            if (post) {
+                team_sum<TPR, 2>(s, red, turn);
+                const float c1 = s[0] * inv, c2 = a.rms ? 0.0f : s[1] * inv;
 #pragma unroll
-            for (int u = 0; u < ITER; ++u)
+                for (int u = 0; u < ITER; ++u)
 #pragma unroll
-                for (int j = 0; j < kVec; ++j) d[u][j] = st.y * (d[u][j] - f[u][j] * c1 - c2);
+                    for (int j = 0; j < kVec; ++j) d[u][j] = r.post.y * (d[u][j] - (r.f[u][j] - r.post.x) * r.post.y * c1 - c2);
+            }
         }
         if (a.dF)
 #pragma unroll
-            for (int u = 0; u < ITER; ++u) store_piece<DT, TPR, VEC>(d[u], a.dF, at, u, t, H);
+            for (int u = 0; u < ITER; ++u) store_piece<DT, TPR, WHOLE>(d[u], a.dF, at, u, t, H);
     };
 
-    if (a.per_wg == 0) {  // a piece of one gate row's rows (all rows where there is no gate)
-        const int64_t group = blockIdx.x / a.pieces, piece = blockIdx.x - group * a.pieces;
-        int64_t r0 = piece * a.rows_per_piece, r1 = r0 + a.rows_per_piece;
-        if (r1 > a.rows_per_gate) r1 = a.rows_per_gate;
-        for (int64_t r = r0 + team; r < r1; r += kTeams) one_row(group * a.rows_per_gate + r, group);
-    } else {              // gate rows of a few rows each: whole ones for a team
-        for (int64_t k = team; k < a.per_wg; k += kTeams) {
-            const int64_t group = (int64_t)blockIdx.x * a.per_wg + k;
-            if (group >= a.groups) break;
-            for (int64_t r = 0; r < a.rows_per_gate; ++r) one_row(group * a.rows_per_gate + r, group);
+    // The rows of this team, one loop for both ways they are dealt (the kernel's code is what a short call waits for): every kTeams-th row of a
+    // piece of one gate row's rows (of all rows where there is no gate), or every kTeams-th gate row of the workgroup's, whole.
+    const bool whole = a.per_wg != 0;
+    const int64_t first_group = whole ? (int64_t)blockIdx.x * a.per_wg : blockIdx.x / a.pieces;
+    const int64_t r0 = whole ? 0 : (blockIdx.x - first_group * a.pieces) * a.rows_per_piece;
+    int64_t r1 = whole ? a.rows_per_gate : r0 + a.rows_per_piece;
+    if (r1 > a.rows_per_gate) r1 = a.rows_per_gate;
+    const int64_t stride = whole ? 1 : kTeams, begin = whole ? 0 : r0 + team;
+    int64_t last_group = whole ? first_group + a.per_wg : first_group + 1;
+    if (last_group > a.groups) last_group = a.groups;
+    int64_t group = whole ? first_group + team : first_group, r = begin;
+    // the next row is on its way while one is worked on, where the registers have room for it
+    constexpr bool kAhead = SIMPLE || TPR == 256;
+    Row cur;
+    bool more = r < r1 && group < last_group;
+    if (kAhead && more) ask(cur, group * a.rows_per_gate + r);
+    while (more) {
+        const int64_t at_group = group, at_row = group * a.rows_per_gate + r;
+        r += stride;
+        const bool end = r >= r1;  // of this team's part of the gate row
+        if (end) {
+            r = begin;
+            group += kTeams;
+        }
+        more = group < last_group && !(end && !whole);
+        if constexpr (kAhead) {
+            Row next;
+            if (more) ask(next, group * a.rows_per_gate + r);
+            one_row(cur, at_row, at_group);
+            cur = next;
+        } else {
+            ask(cur, at_row);
+            one_row(cur, at_row, at_group);
+        }
+        if (whole && end) {
             if (a.dgate)
 #pragma unroll
-                for (int u = 0; u < ITER; ++u) store_piece<BSP_F32, TPR, VEC>(acc[kDgate][u], a.dgate, group * H, u, t, H);
+                for (int u = 0; u < ITER; ++u) store_piece<BSP_F32, TPR, WHOLE>(acc[kDgate][u], a.dgate, at_group * H, u, t, H);
             clear(kDgate);
         }
     }
     // the workgroup's sums: the teams' in ascending order, a piece at a time through LDS
-    for (int i = 0; i < kSums; ++i) {
-        if (!((a.want >> i) & 1u)) continue;
-        float v[ITER][kVec];
-#pragma unroll
-        for (int u = 0; u < ITER; ++u)
-#pragma unroll
-            for (int j = 0; j < kVec; ++j)
-                v[u][j] = i == 0 ? acc[0][u][j] : (i == 1 ? acc[1][u][j] : (i == 2 ? acc[2][u][j] : (i == 3 ? acc[3][u][j] : acc[4][u][j])));
+    static_for<0, kSums>([&](auto kind) {
+        constexpr int i = decltype(kind)::value;
+        if (SIMPLE && i != kDwPre && i != kDbPre) return;
+        if (!((a.want >> i) & 1u)) return;  // uniform
         float *out = a.sums + ((int64_t)i * gridDim.x + blockIdx.x) * H;
 #pragma unroll
         for (int u = 0; u < ITER; ++u) {
+            float(&v)[kVec] = acc[i][u];
             if constexpr (kTeams > 1) {
                 __syncthreads();
                 if (team)
 #pragma unroll
-                    for (int j = 0; j < kVec; ++j) share[((team - 1) * kVec + j) * TPR + t] = v[u][j];
+                    for (int j = 0; j < kVec; ++j) share[((team - 1) * kVec + j) * TPR + t] = v[j];
                 __syncthreads();
                 if (!team)
 #pragma unroll
                     for (int o = 0; o < kTeams - 1; ++o)
 #pragma unroll
-                        for (int j = 0; j < kVec; ++j) v[u][j] += share[(o * kVec + j) * TPR + t];
+                        for (int j = 0; j < kVec; ++j) v[j] += share[(o * kVec + j) * TPR + t];
             }
-            if (!team) store_piece<BSP_F32, TPR, VEC>(v[u], out, 0, u, t, H);
+            if (!team) store_piece<BSP_F32, TPR, WHOLE>(v, out, 0, u, t, H);
         }
-    }
+    });
 }
 
 // out[k][row][c] = sum over `n` workgroups' sums, ascending in each of 16 interleaved parts, then the parts.
@@ -441,7 +514,7 @@ struct Deal {
 
 Deal deal(int64_t T, int64_t H, int64_t gate_rows) {
     Deal d;
-    const int64_t teams = H <= 1024 ? 4 : 1;
+    const int64_t teams = H <= 1024 ? kBackTeams : 1;
     d.groups = (int32_t)(gate_rows > 0 ? gate_rows : 1);
     d.rows_per_gate = T / d.groups;
     int64_t rows = (T + kRanges - 1) / kRanges;
@@ -469,23 +542,25 @@ int check(int64_t T, int64_t H, int dt, int norms, int kind, const void *gate, i
     return BSP_OK;
 }
 
-template <typename... P>
-bool vectors(int64_t H, P... p) {
-    return H % kVec == 0 && (aligned(p, 16) && ...);
-}
-
 template <int DT, int TPR, int ITER>
-void launch_forward(const Forward &a, bool vec, hipStream_t s) {
+void launch_forward(const Forward &a, hipStream_t s) {
     constexpr int kTeams = TPR < 256 ? 256 / TPR : 1;
     const unsigned grid = (unsigned)((a.T + kTeams - 1) / kTeams);
-    if (vec) block_norm_kernel<DT, TPR, ITER, true><<<grid, TPR < 256 ? 256 : TPR, 0, s>>>(a);
+    if (a.width % kVec == 0) block_norm_kernel<DT, TPR, ITER, true><<<grid, TPR < 256 ? 256 : TPR, 0, s>>>(a);
     else block_norm_kernel<DT, TPR, ITER, false><<<grid, TPR < 256 ? 256 : TPR, 0, s>>>(a);
 }
 
 template <int DT, int TPR, int ITER>
-void launch_backward(const Backward &a, bool vec, unsigned grid, hipStream_t s) {
-    if (vec) block_norm_back_kernel<DT, TPR, ITER, true><<<grid, TPR < 256 ? 256 : TPR, 0, s>>>(a);
-    else block_norm_back_kernel<DT, TPR, ITER, false><<<grid, TPR < 256 ? 256 : TPR, 0, s>>>(a);
+void launch_backward(const Backward &a, unsigned grid, hipStream_t s) {
+    constexpr int kThreads = TPR == 64 ? 64 * kBackTeams : TPR;
+    const bool simple = a.norms == BSP_NORM_PRE && !a.gate;
+    if (a.width % kVec == 0) {
+        if (simple) block_norm_back_kernel<DT, TPR, ITER, true, true><<<grid, kThreads, 0, s>>>(a);
+        else block_norm_back_kernel<DT, TPR, ITER, true, false><<<grid, kThreads, 0, s>>>(a);
+    } else {
+        if (simple) block_norm_back_kernel<DT, TPR, ITER, false, true><<<grid, kThreads, 0, s>>>(a);
+        else block_norm_back_kernel<DT, TPR, ITER, false, false><<<grid, kThreads, 0, s>>>(a);
+    }
 }
 
 }  // namespace
@@ -506,14 +581,13 @@ extern "C" int bsp_block_norm(const void *X, const void *F, int dt, int64_t T, i
     if (!aligned(stats_post, 8) || !aligned(stats_pre, 8)) return BSP_ERR_SHAPE;
     const Forward a = {X, F, gate, w_post, b_post, w_pre, b_pre, Z, Hn, stats_post, stats_pre,
                        T, gate ? T / gate_rows : T, x_scale, eps, (int32_t)H, kind == BSP_NORM_RMS, norms};
-    const bool vec = vectors(H, X, F, gate, w_post, b_post, w_pre, b_pre, Z, Hn);
     hipStream_t s = (hipStream_t)stream;
     BSP_DISPATCH_DTYPE(dt, DT, {
-        if (H <= 512) launch_forward<DT, 64, 1>(a, vec, s);
-        else if (H <= 1024) launch_forward<DT, 64, 2>(a, vec, s);
-        else if (H <= 2048) launch_forward<DT, 64, 4>(a, vec, s);
-        else if (H <= 4096) launch_forward<DT, 256, 2>(a, vec, s);
-        else launch_forward<DT, 256, 4>(a, vec, s);
+        if (H <= 512) launch_forward<DT, 64, 1>(a, s);
+        else if (H <= 1024) launch_forward<DT, 64, 2>(a, s);
+        else if (H <= 2048) launch_forward<DT, 64, 4>(a, s);
+        else if (H <= 4096) launch_forward<DT, 256, 2>(a, s);
+        else launch_forward<DT, 256, 4>(a, s);
     });
     return check_launch();
 }
@@ -559,13 +633,12 @@ extern "C" int bsp_block_norm_backward(const void *dZ, const void *dH, const voi
                       kind == BSP_NORM_RMS, norms, d.pieces, d.groups, d.per_wg, 0};
         for (int i = 0; i < kSums; ++i)
             if (c.out[i] && !(direct && i == kDgate)) a.want |= 1u << i;
-        const bool vec = vectors(H, dZ, a.dH, a.Z, a.F, gate, w_post, b_post, w_pre, dX, dF, direct ? dgate : nullptr);
         BSP_DISPATCH_DTYPE(dt, DT, {
-            if (H <= 512) launch_backward<DT, 64, 1>(a, vec, (unsigned)d.wgs, s);
-            else if (H <= 1024) launch_backward<DT, 64, 2>(a, vec, (unsigned)d.wgs, s);
-            else if (H <= 2048) launch_backward<DT, 256, 1>(a, vec, (unsigned)d.wgs, s);
-            else if (H <= 4096) launch_backward<DT, 256, 2>(a, vec, (unsigned)d.wgs, s);
-            else launch_backward<DT, 512, 2>(a, vec, (unsigned)d.wgs, s);
+            if (H <= 512) launch_backward<DT, 64, 1>(a, (unsigned)d.wgs, s);
+            else if (H <= 1024) launch_backward<DT, 64, 2>(a, (unsigned)d.wgs, s);
+            else if (H <= 2048) launch_backward<DT, 256, 1>(a, (unsigned)d.wgs, s);
+            else if (H <= 4096) launch_backward<DT, 256, 2>(a, (unsigned)d.wgs, s);
+            else launch_backward<DT, 512, 2>(a, (unsigned)d.wgs, s);
         });
         if (int st = check_launch()) return st;
     }

@@ -49,13 +49,13 @@ struct Piece {
     }
 };
 
-// One row segment per 16 lanes, kRowsEach of them in a column of segments, all asked for at once.
+// One row segment per 16 lanes, kRowsEach of them one below the other, all asked for at once.
 constexpr int kRowsEach = 2;
 
 template <int DT>
 __global__ __launch_bounds__(kThreads) void quant_rows_kernel(Quant a) {
     const int c0 = 8 * (threadIdx.x & 15);
-    const int64_t strips = (a.rows + kRowsEach * 16 - 1) / (kRowsEach * 16), tc = blockIdx.x / strips, strip = blockIdx.x - tc * strips;
+    const int64_t strip = blockIdx.x / a.tiles_c, tc = blockIdx.x - strip * a.tiles_c;  // (along the rows first)
     const int64_t row0 = strip * (kRowsEach * 16) + (threadIdx.x >> 4), col0 = 128 * tc + c0;
     const int cols = a.cols - col0 > 8 ? 8 : (int)(a.cols - col0);
     Piece<DT> v[kRowsEach];
@@ -67,8 +67,7 @@ __global__ __launch_bounds__(kThreads) void quant_rows_kernel(Quant a) {
         float m = 0.0f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) m = __builtin_fmaxf(m, magnitude(v[i][j]));
-#pragma unroll
-        for (int d = 1; d < 16; d <<= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d));
+        m = max_of_16(m);
         if (row >= a.rows) continue;
         const uint32_t e = scale_exponent(m);
         const float s = inverse_scale(e);
@@ -119,8 +118,7 @@ __global__ __launch_bounds__(kThreads) void quant_kernel(Quant a) {
             float m = 0.0f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) m = __builtin_fmaxf(m, magnitude(v[i][j]));
-#pragma unroll
-            for (int d = 1; d < 16; d <<= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d));
+            m = max_of_16(m);
             e_row[i] = scale_exponent(m);
             if (a.Q && (tid & 15) == 0 && i < rows) a.S[(row0 + i) * a.tiles_c + tc] = (uint8_t)e_row[i];
         }

@@ -13,6 +13,13 @@ __device__ __forceinline__ float magnitude(float x) {
     return u < 0x7f800000u ? __uint_as_float(u) : 0.0f;
 }
 
+// The largest of 16 lanes' values (all >= 0), in every one of them: rotations within the row.
+template <int CTRL>
+__device__ __forceinline__ float max_turned(float x) {
+    return __builtin_fmaxf(x, __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, false)));
+}
+__device__ __forceinline__ float max_of_16(float x) { return max_turned<0x128>(max_turned<0x124>(max_turned<0x122>(max_turned<0x121>(x)))); }
+
 // The biased exponent of the least power of two 2^e with largest / 2^e <= 448 = 1.75 2^8 (not below 2^-127; 2^0 for zero).
 __device__ __forceinline__ uint32_t scale_exponent(float largest) {
     const uint32_t u = __float_as_uint(largest);

@@ -130,46 +130,90 @@ __global__ __launch_bounds__(64 * WA * WB) void fp8_tile_kernel(Product p) {
         if (first + n < last) load(first + n, n);  // uniform
     });
     const uint32_t scale_a = kCodes + (uint32_t)(wa * FA * 32 + l32) * 4, scale_b = kCodes + (uint32_t)(TA + wb * FB * 32 + l32) * 4;
-    int slot = 0;
-    for (int s = first; s < last; ++s) {
-        // this step's loads are done where no more are left than those of the NS - 2 steps behind it; at the end there are fewer
-        if (NS > 2 && s + NS - 1 < last + 1) wait_loads<(NS - 2) * (kLoads + kScaleLoads)>();
-        else wait_loads<0>();
-        barrier();  // this step is in LDS, and nobody reads the slot before it any more
-        if (s + NS - 1 < last) load(s + NS - 1, slot == 0 ? NS - 1 : slot - 1);
-        uint32_t sc[FA + FB];
+    struct Operands {
+        i32x8 a[FA], b[FB];
+    };
+    uint32_t sc[FA + FB];
+    auto read_scales = [&](int slot) {
 #pragma unroll
         for (int f = 0; f < FA + FB; ++f)
             sc[f] = *reinterpret_cast<const uint32_t *>(smem + slot * kStage + (f < FA ? scale_a + 128 * f : scale_b + 128 * (f - FA)));
+    };
+    auto read = [&](Operands &o, int slot, int sub) {
 #pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-            i32x8 a[FA], b[FB];
+        for (int i = 0; i < FA; ++i) o.a[i] = operand(cell_a, slot, i, sub);
 #pragma unroll
-            for (int i = 0; i < FA; ++i) a[i] = operand(cell_a, slot, i, sub);
+        for (int j = 0; j < FB; ++j) o.b[j] = operand(cell_b, slot, j, sub);
+    };
+    auto multiply = [&](const Operands &o) {
+        if constexpr (DT == BSP_F32) {
+            static_for<0, 4>([&](auto kk) {
+                constexpr int k = 2 * decltype(kk)::value;
+                uint4 wa8[FA], wb8[FB];
 #pragma unroll
-            for (int j = 0; j < FB; ++j) b[j] = operand(cell_b, slot, j, sub);
-            if constexpr (DT == BSP_F32) {
-                static_for<0, 4>([&](auto kk) {
-                    constexpr int k = 2 * decltype(kk)::value;
-                    uint4 wa8[FA], wb8[FB];
+                for (int i = 0; i < FA; ++i) wa8[i] = widen8((uint32_t)o.a[i][k], (uint32_t)o.a[i][k + 1], sc[i]);
 #pragma unroll
-                    for (int i = 0; i < FA; ++i) wa8[i] = widen8((uint32_t)a[i][k], (uint32_t)a[i][k + 1], sc[i]);
-#pragma unroll
-                    for (int j = 0; j < FB; ++j) wb8[j] = widen8((uint32_t)b[j][k], (uint32_t)b[j][k + 1], sc[FA + j]);
-#pragma unroll
-                    for (int i = 0; i < FA; ++i)
-#pragma unroll
-                        for (int j = 0; j < FB; ++j) acc[i][j] = mfma32<BSP_BF16>(wa8[i], wb8[j], acc[i][j]);
-                });
-            } else {
+                for (int j = 0; j < FB; ++j) wb8[j] = widen8((uint32_t)o.b[j][k], (uint32_t)o.b[j][k + 1], sc[FA + j]);
 #pragma unroll
                 for (int i = 0; i < FA; ++i)
 #pragma unroll
-                    for (int j = 0; j < FB; ++j) acc[i][j] = mfma_scaled(a[i], b[j], acc[i][j], sc[i], sc[FA + j]);
-            }
+                    for (int j = 0; j < FB; ++j) acc[i][j] = mfma32<BSP_BF16>(wa8[i], wb8[j], acc[i][j]);
+            });
+        } else {
+#pragma unroll
+            for (int i = 0; i < FA; ++i)
+#pragma unroll
+                for (int j = 0; j < FB; ++j) acc[i][j] = mfma_scaled(o.a[i], o.b[j], acc[i][j], sc[i], sc[FA + j]);
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        slot = slot == NS - 1 ? 0 : slot + 1;
+    };
+    constexpr int kEach = kLoads + kScaleLoads;
+    int slot = 0;
+    if constexpr (NS == 2) {
+        for (int s = first; s < last; ++s) {
+            wait_loads<0>();
+            barrier();  // this step is in LDS, and nobody reads the other slot any more
+            if (s + 1 < last) load(s + 1, slot ^ 1);
+            read_scales(slot);
+#pragma unroll
+            for (int sub = 0; sub < 2; ++sub) {
+                Operands o;
+                read(o, slot, sub);
+                multiply(o);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            slot ^= 1;
+        }
+    } else {
+        // The first half of a step is read while the second half of the one before it is multiplied: a step is in LDS, for everybody, half a
+        // step before its turn.
+        Operands o[2];
+        if (first + NS - 1 <= last) wait_loads<(NS - 2) * kEach>();
+        else wait_loads<0>();
+        barrier();
+        read_scales(0);
+        read(o[0], 0, 0);
+        // (The products stay on their side of the barrier: the compiler would move them behind it, where everything waits for everything.)
+        auto step = [&](int s, auto behind) {  // behind: whether all the steps that the ring has room for are behind this one
+            constexpr bool kFull = decltype(behind)::value;
+            const int next = slot == NS - 1 ? 0 : slot + 1;
+            if (kFull) load(s + NS - 1, slot == 0 ? NS - 1 : slot - 1);
+            read(o[1], slot, 1);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(o[0]);
+            __builtin_amdgcn_sched_barrier(0);
+            // the next step's loads are done where no more are left than those of the steps behind it
+            wait_loads<kFull ? (NS - 2) * kEach : 0>();
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            barrier();
+            if (kFull || s + 1 < last) read(o[0], next, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(o[1]);
+            if (kFull || s + 1 < last) read_scales(next);
+            slot = next;
+        };
+        int s = first;
+        for (; s + NS - 1 < last; ++s) step(s, std::true_type{});
+        for (; s < last; ++s) step(s, std::false_type{});
     }
 
     // 16-bit results without a residual: finished where they are, rounded into a tile of all tokens in LDS, and out in whole rows.
@@ -395,25 +439,28 @@ constexpr int64_t kFewTokens = 32;  // of fp8_few_kernel
 bool quantised_inside(int64_t T, int64_t steps) { return T <= 16 ? steps <= 2 * kFewWaves : T <= kFewTokens && steps <= kFewWaves; }
 
 struct Shape {
-    int tile;    // 256, 128, 64, or 63: 64 with its steps four deep in LDS; 0: few tokens
+    int tile;    // 256, 128, 64; 127 and 63: 128 and 64 with their steps three and four deep in LDS; 0: few tokens
     int splits, split_steps;
 };
 
-// Microseconds of a product in tiles of `tile` x `tile`, `n` of them (with the splits), of `steps` steps; fitted to 60 shapes of 32 to 16384 rows
-// and 1024 to 16384 columns.  `wide`: fp32 results, whose instructions take twice as long.  A larger tile loads less for a product, but its
-// workgroups leave compute units idle at the end of a round, and one of 256 x 256 fills a compute unit, so that its epilogue (GELU: 6 us a round)
-// hides nothing.  Measured, 256 / 128 / 64 / 63: 16384 x 4096, K = 4096 234 / 268 / 418 / 463; 8192 x 4096, K = 1024 43 / 45 / 62 / 77, with GELU
-// 57 / 53 / 68; 8192 x 1024, K = 4096 50 / 37 / 59 / 62; 1024 x 1024, K = 1024 19 / 9.1 / 7.8 / 7.9; 512 x 1024, K = 4096 53 / 27 / 20 / 12.5.
+// Microseconds of a product in `n` tiles (with the splits) of `steps` steps; fitted to 60 shapes of 32 to 16384 rows and 1024 to 16384
+// columns.  `wide`: fp32 results, whose instructions take twice as long.  A larger tile loads less for a product, but its
+// workgroups leave compute units idle at the end of a round, and one of 256 x 256 fills a compute unit, so that its epilogue (GELU: 8 us a round)
+// hides nothing.  Two steps in LDS let two workgroups of 128 x 128 share a compute unit and wait for each other; with three
+// a workgroup that is alone on it reads half a step ahead.  Measured, 256 / 128 / 127 / 64 / 63: 16384 x 4096, K = 4096 234 / 268 / - / 418 / -; 8192 x
+// 4096, K = 1024 45 / 47 / 62 / 63 / 79, with GELU 58 / 53 / - / 68; 2048 x 1024, K = 4096 50 / 27 / 19 / 20 / 18; 512 x 1024, K = 4096 50 / 26 / 19 / 20 /
+// 11.9; 1024 x 4096, K = 8192 in fp32 166 / 82 / 72 / 88 / 92.
 double tile_us(int tile, double n, double steps, bool wide, bool gelu) {
-    const double rounds256 = __builtin_ceil(n / 256.0);
-    if (tile == 256) return 5.0 + rounds256 * ((wide ? 3.2 : 1.62) * steps + 5.0 + (gelu ? 6.0 : 0.0));
-    if (tile == 128) {
-        if (n <= 256.0) return 5.0 + (wide ? 1.12 : 0.72) * steps + (gelu ? 2.5 : 0.0);
-        return 3.5 + __builtin_ceil(n / 512.0) * ((wide ? 1.85 : 1.03) * steps + 2.2 + (gelu ? 2.5 : 0.0));
+    const double rounds = __builtin_ceil(n / 256.0), pairs = __builtin_ceil(n / 512.0);
+    switch (tile) {
+        case 256: return 5.0 + rounds * ((wide ? 3.2 : 1.62) * steps + 5.0 + (gelu ? 8.5 : 0.0));
+        case 128: return 3.5 + pairs * ((wide ? 1.85 : 1.03) * steps + 2.2 + (gelu ? 2.5 : 0.0));
+        case 127: return 3.5 + rounds * ((wide ? 1.04 : 0.46) * steps + 1.5 + (gelu ? 2.5 : 0.0));
+        case 64: return 3.5 + __builtin_ceil(n / 1024.0) * ((wide ? 1.25 : 0.83) * steps + 1.6 + (gelu ? 1.0 : 0.0));
+        default:
+            if (n <= 256.0) return 5.0 + (wide ? 0.41 : 0.215) * steps;
+            return 3.5 + pairs * ((wide ? 0.75 : 0.41) * steps + 1.8 + (gelu ? 0.5 : 0.0));
     }
-    if (tile == 64) return 3.5 + __builtin_ceil(n / 1024.0) * ((wide ? 1.25 : 0.83) * steps + 1.6 + (gelu ? 1.0 : 0.0));
-    if (n <= 256.0) return 5.5 + (wide ? 0.48 : 0.23) * steps;
-    return 3.5 + __builtin_ceil(n / 512.0) * ((wide ? 0.8 : 0.44) * steps + 2.2 + (gelu ? 0.5 : 0.0));
 }
 
 // The tile, and into how many runs the steps are split where there are too few tiles for the compute units (256 x 256, K = 16384 in fp32: 60 us,
@@ -422,8 +469,8 @@ Shape choose(int64_t T, int64_t M, int64_t steps, bool wide, bool gelu) {
     Shape best = {0, 1, (int)steps};
     if (T <= kFewTokens) return best;
     double least = 0.0;
-    for (int tile : {256, 128, 64, 63}) {
-        const double side = tile == 63 ? 64.0 : (double)tile, n = __builtin_ceil((double)T / side) * __builtin_ceil((double)M / side);
+    for (int tile : {256, 128, 127, 64, 63}) {
+        const double side = (double)((tile + 1) / 2 * 2), n = __builtin_ceil((double)T / side) * __builtin_ceil((double)M / side);
         for (int k = 1; k <= 16; k *= 2) {
             if (k > 1 && (steps < 4 * k || n * k > 512.0)) break;
             const int64_t each = (steps + k - 1) / k;
@@ -469,6 +516,7 @@ int launch_product(const Product &p, const Shape &c, hipStream_t s) {
     if (c.tile == 0) return launch_few<DT, false>(p, nullptr, 0, s);
     if (c.tile == 256) st = launch_tile<DT, 2, 4, 4, 2, 2>(p, c.splits, s);
     else if (c.tile == 128) st = launch_tile<DT, 2, 1, 2, 4, 2>(p, c.splits, s);
+    else if (c.tile == 127) st = launch_tile<DT, 2, 1, 2, 4, 3>(p, c.splits, s);
     else if (c.tile == 64) st = launch_tile<DT, 1, 1, 2, 2, 2>(p, c.splits, s);
     else st = launch_tile<DT, 1, 1, 2, 2, 4>(p, c.splits, s);
     if (st || c.splits == 1) return st;
