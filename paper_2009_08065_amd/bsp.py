@@ -656,71 +656,30 @@ NORM_LAYER, NORM_RMS = 0, 1
 NORM_POST, NORM_PRE = 1, 2
 
 
-def _norm_fits(like, rows, vectors, gate):
-    T, H = like.shape
-    for x in rows:
-        if x is not None and (x.dtype != like.dtype or x.shape != like.shape):
-            raise ValueError("the [T, H] tensors must share one shape and dtype")
-    for x in vectors:
-        if x is not None and (x.dtype != like.dtype or x.numel() != H):
-            raise ValueError("weights and biases must have H elements of the dtype of the rows")
-    if gate is None:
-        return 0
-    if gate.dtype != like.dtype or gate.dim() not in (1, 2) or gate.shape[-1] != H:
-        raise ValueError("gate must be [gate_rows, H] of the dtype of the rows")
-    return gate.numel() // H
-
-
 def bsp_block_norm(X, F=None, norms=NORM_PRE, kind=NORM_LAYER, eps=1e-12, x_scale=1.0, gate=None, w_post=None, b_post=None, w_pre=None,
                    b_pre=None, Z=None, H=None, want=("Z", "stats_post", "stats_pre")):
     """Z = x_scale X + gate * N_post(F), H = N_pre(Z) (norms: NORM_POST, NORM_PRE or both).  Returns (Z, H, stats_post, stats_pre);
     what is absent or not in `want` (and not passed) is None, without NORM_PRE also H."""
-    native = _native()
-    _here(X, F, gate, w_post, b_post, w_pre, b_pre, Z, H)
-    T, width = X.shape
-    gate_rows = _norm_fits(X, (F, Z, H), (w_post, b_post, w_pre, b_pre), gate)
-    dt = _DT[X.dtype]
-    if Z is None and ("Z" in want or not norms & NORM_PRE):
-        Z = native.empty(X, dt, T, width)
-    if H is None and norms & NORM_PRE:
-        H = native.empty(X, dt, T, width)
-    stats_post = native.empty(X, F32, T, 2) if norms & NORM_POST and "stats_post" in want else None
-    stats_pre = native.empty(X, F32, T, 2) if norms & NORM_PRE and "stats_pre" in want else None
-    st = native.bsp_block_norm(X, F, dt, T, width, norms, kind, eps, x_scale, gate, gate_rows, w_post, b_post, w_pre, b_pre, Z, H,
-                               stats_post, stats_pre, _stream())
+    bits = ("Z" in want) | ("stats_post" in want) << 1 | ("stats_pre" in want) << 2
+    st, Z, H, stats_post, stats_pre = _native().block_norm(X, F, norms, kind, eps, x_scale, gate, w_post, b_post, w_pre, b_pre, Z, H, bits,
+                                                           torch._C._cuda_getDevice(), _stream())
     _check(st, "bsp_block_norm")
     return Z, H, stats_post, stats_pre
 
 
+_NORM_GRADIENTS = ("dx", "df", "dw_post", "db_post", "dw_pre", "db_pre", "dgate")
+
+
 def bsp_block_norm_backward(dZ, dH, Z, F=None, norms=NORM_PRE, kind=NORM_LAYER, x_scale=1.0, gate=None, w_post=None, b_post=None,
                             w_pre=None, b_pre=None, stats_post=None, stats_pre=None, dX=None, dF=None,
-                            want=("dx", "df", "dw_post", "db_post", "dw_pre", "db_pre", "dgate"), ws=None):
+                            want=_NORM_GRADIENTS, ws=None):
     """Gradients of bsp_block_norm, as a dict of those in `want` that the call has (the others None): dx and df in the dtype of the
     rows, the sums over the rows in fp32.  dZ, or dH and Z, may be None where the forward pass had no use for them."""
-    native = _native()
-    _here(dZ, dH, Z, F, gate, w_post, b_post, w_pre, b_pre, stats_post, stats_pre, dX, dF, ws)
-    like = dZ if dZ is not None else dH
-    T, H = like.shape
-    gate_rows = _norm_fits(like, (dZ, dH, Z, F, dX, dF), (w_post, b_post, w_pre, b_pre), gate)
-    for stats in (stats_post, stats_pre):
-        if stats is not None and tuple(stats.shape) != (T, 2):
-            raise ValueError("stats must be [T, 2]")
-    dt = _DT[like.dtype]
-    out = {"dx": dX, "df": dF}
-    for name in ("dx", "df"):
-        if out[name] is None and name in want:
-            out[name] = native.empty(like, dt, T, H)
-    for name, place, x in (("dw_post", NORM_POST, w_post), ("db_post", NORM_POST, b_post), ("dw_pre", NORM_PRE, w_pre), ("db_pre", NORM_PRE, b_pre)):
-        out[name] = native.empty(like, F32, H) if x is not None and norms & place and name in want else None
-    out["dgate"] = native.empty(like, F32, gate_rows, H) if gate is not None and "dgate" in want else None
-    need = native.bsp_block_norm_backward_workspace_bytes(T, H, gate_rows)
-    if ws is None and any(out[k] is not None for k in ("dw_post", "db_post", "dw_pre", "db_pre", "dgate")):
-        ws = native.empty(like, _U8, need)
-    st = native.bsp_block_norm_backward(dZ, dH, Z, F, dt, T, H, norms, kind, x_scale, gate, gate_rows, w_post, b_post, w_pre, stats_post,
-                                        stats_pre, out["dx"], out["df"], out["dw_post"], out["db_post"], out["dw_pre"], out["db_pre"],
-                                        out["dgate"], ws, 0 if ws is None else ws.numel() * ws.element_size(), _stream())
-    _check(st, "bsp_block_norm_backward")
-    return out
+    bits = 127 if want is _NORM_GRADIENTS else sum((name in want) << i for i, name in enumerate(_NORM_GRADIENTS))
+    out = _native().block_norm_backward(dZ, dH, Z, F, norms, kind, x_scale, gate, w_post, b_post, w_pre, b_pre, stats_post, stats_pre, dX, dF, bits,
+                                        ws, torch._C._cuda_getDevice(), _stream())
+    _check(out[0], "bsp_block_norm_backward")
+    return dict(zip(_NORM_GRADIENTS, out[1:]))
 
 
 def bsp_compression_rate(M, N, R, kept_cols_total) -> float:
