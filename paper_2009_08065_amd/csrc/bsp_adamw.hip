@@ -23,10 +23,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxTensors = 40;            // 40 entries of 88 bytes: a launch has 4 KB of arguments
-constexpr int kPerThread = 8;              // elements (fp32 moments), 256 apart
 constexpr int kBlock = 256;                // elements of an 8-bit scale: one wavefront, 4 per lane
 constexpr int kBlocksPerWave = 4;
-constexpr int64_t kChunk32 = kThreads * kPerThread, kChunk8 = (kThreads / kWave) * kBlocksPerWave * kBlock;
+constexpr int64_t kChunk8 = (kThreads / kWave) * kBlocksPerWave * kBlock;
 
 struct Entry {
     float *w;
@@ -131,21 +130,23 @@ __device__ __forceinline__ void store_copy(void *p, int64_t i, float v) {
     if (p) elem<CDT>::store(p, i, v);
 }
 
-template <int GDT, int CDT>
+// PER: elements of a thread, 256 apart.  Four for large models (302 M weights 1889 us, with eight 1974); two where the launch would have few workgroups (750000 weights of 12 tensors:
+// 10.4 us with eight).
+template <int GDT, int CDT, int PER>
 __global__ __launch_bounds__(kThreads) void adamw32_kernel(Table tab, Hyper h) {
     Step s;
     if (!begin_step(h, s)) return;
     const int k = find_tensor(tab);
     const Entry &e = tab.e[k];
-    const int64_t base = (int64_t)(blockIdx.x - tab.first[k]) * kChunk32;
+    const int64_t base = (int64_t)(blockIdx.x - tab.first[k]) * (kThreads * PER);
     float *w = e.w + base, *m = (float *)e.m + base, *v = (float *)e.v + base;
     const int64_t left = e.n - base;
     const bool grouped = e.keep || e.alpha;
     Groups groups(e, grouped ? base : 0);
     if (grouped) groups.advance(threadIdx.x);
     const float decay = s.lr * e.decay;
-#pragma unroll 4
-    for (int j = 0; j < kPerThread; ++j) {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
         const uint32_t i = j * kThreads + threadIdx.x;
         if (i >= left) break;
         const float w0 = w[i];
@@ -185,19 +186,21 @@ __device__ __forceinline__ uint32_t mix(uint32_t x) {
     return x ^ (x >> 16);
 }
 
-// The largest of 64 lanes' values (all >= 0), in every lane: within rows of 16 lanes and then across them, without LDS.
+// The largest of 64 lanes' values (all >= 0, as their bits, whose order is theirs), in every lane: within rows of 16 lanes and then across them,
+// without LDS.
 template <int CTRL, int ROWS>
-__device__ __forceinline__ float max_dpp(float x) {
-    return __builtin_fmaxf(x, __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, ROWS, 0xf, false)));
+__device__ __forceinline__ uint32_t max_dpp(uint32_t x) {
+    const uint32_t y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+    return x > y ? x : y;
 }
-__device__ __forceinline__ float wave_max(float x) {
+__device__ __forceinline__ float wave_max(uint32_t x) {
     x = max_dpp<0x111, 0xf>(x);  // row_shr 1, 2, 4, 8: lane 15 of a row has the row's
     x = max_dpp<0x112, 0xf>(x);
     x = max_dpp<0x114, 0xf>(x);
     x = max_dpp<0x118, 0xf>(x);
     x = max_dpp<0x142, 0xa>(x);  // row_bcast 15 into rows 1 and 3, 31 into rows 2 and 3
     x = max_dpp<0x143, 0xc>(x);
-    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), 63));
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)x, 63));
 }
 
 // |y| <= 448 to one of the two codes' values next to it, up where the 16 bits (of 2^16) exceed what is missing.  Below 2^-6 the
@@ -292,7 +295,7 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(Table tab, Hyper h) {
                 }
             }
         }
-        float top_m = 0.0f, top_r = 0.0f;
+        uint32_t bits_m = 0, bits_r = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             float x = g[j];
@@ -310,14 +313,14 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(Table tab, Hyper h) {
             }
             wn = wn - rate * m[j] * __builtin_amdgcn_rcpf(__builtin_fmaf(r[j], root, h.eps));
             w[j] = (kept >> j) & 1u ? wn : 0.0f;
-            top_m = __builtin_fmaxf(top_m, __builtin_fabsf(m[j]));
-            top_r = __builtin_fmaxf(top_r, r[j]);
+            const uint32_t um = __float_as_uint(m[j]) & 0x7fffffffu, ur = __float_as_uint(r[j]);
+            bits_m = bits_m > um ? bits_m : um;
+            bits_r = bits_r > ur ? bits_r : ur;
         }
-        top_m = wave_max(top_m);
-        top_r = wave_max(top_r);
+        const float top_m = wave_max(bits_m), top_r = wave_max(bits_r);
         // (2^-100: below it 448 / largest has no number, and such moments move nothing)
         const bool has_m = top_m >= 0x1p-100f, has_r = top_r >= 0x1p-100f;
-        const float im = has_m ? 448.0f / top_m : 0.0f, ir = has_r ? 448.0f / top_r : 0.0f;
+        const float im = has_m ? 448.0f * __builtin_amdgcn_rcpf(top_m) : 0.0f, ir = has_r ? 448.0f * __builtin_amdgcn_rcpf(top_r) : 0.0f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const uint32_t bits = mix((uint32_t)(i0 + j) + s.salt);
@@ -350,15 +353,11 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(Table tab, Hyper h) {
     }
 }
 
-template <int GDT>
-void launch(const Table &tab, const Hyper &h, unsigned wgs, int bits, int cdt, hipStream_t s) {
-    if (bits == 32) {
-        if (cdt == BSP_F16) adamw32_kernel<GDT, BSP_F16><<<wgs, kThreads, 0, s>>>(tab, h);
-        else adamw32_kernel<GDT, BSP_BF16><<<wgs, kThreads, 0, s>>>(tab, h);
-    } else {
-        if (cdt == BSP_F16) adamw8_kernel<GDT, BSP_F16><<<wgs, kThreads, 0, s>>>(tab, h);
-        else adamw8_kernel<GDT, BSP_BF16><<<wgs, kThreads, 0, s>>>(tab, h);
-    }
+template <int GDT, int CDT>
+void launch(const Table &tab, const Hyper &h, unsigned wgs, int bits, int per, hipStream_t s) {
+    if (bits == 8) adamw8_kernel<GDT, CDT><<<wgs, kThreads, 0, s>>>(tab, h);
+    else if (per == 4) adamw32_kernel<GDT, CDT, 4><<<wgs, kThreads, 0, s>>>(tab, h);
+    else adamw32_kernel<GDT, CDT, 2><<<wgs, kThreads, 0, s>>>(tab, h);
 }
 
 // Whether two tensors' weights share memory (a tied tensor that is listed twice would be updated by two workgroups at once).
@@ -397,19 +396,24 @@ extern "C" int bsp_adamw_step(const bsp_adamw_tensor *tensors, int64_t count, in
     if (count && !tensors) return BSP_ERR_NULL;
     if (!valid_dtype(gdt) || (cdt != BSP_BF16 && cdt != BSP_F16)) return BSP_ERR_DTYPE;
     if (!lr_t && t < 1) return BSP_ERR_SHAPE;
-    const int64_t chunk = state_bits == 32 ? kChunk32 : kChunk8;
+    const int64_t largest = state_bits == 32 ? kThreads * 4 : kChunk8;
+    int64_t all = 0;
     for (int64_t i = 0; i < count; ++i) {  // all of them before the first launch
         const bsp_adamw_tensor &x = tensors[i];
         if (x.M < 0 || x.N < 0 || x.N > 0x7fffffff || (x.M && x.N > 0x7fffffffffffll / x.M)) return BSP_ERR_SHAPE;
         if (x.M == 0 || x.N == 0) continue;
         if (!x.w || !x.g || !x.m || !x.v || (state_bits == 8 && !x.scales)) return BSP_ERR_NULL;
         if ((x.keep || x.alpha) && (x.R <= 0 || x.M % x.R != 0)) return BSP_ERR_SHAPE;
-        if ((x.M * x.N + chunk - 1) / chunk >= ((int64_t)1 << 31)) return BSP_ERR_SHAPE;
+        const int64_t n = (x.M * x.N + largest - 1) / largest;
+        if (n >= ((int64_t)1 << 31)) return BSP_ERR_SHAPE;
+        all += n;
         if (!aligned(x.w, 4) || !aligned(x.g, dtype_size(gdt)) || (state_bits == 32 && (!aligned(x.m, 4) || !aligned(x.v, 4))) ||
             !aligned(x.scales, 4) || !aligned(x.copy, 2) || !aligned(x.alpha, 4))
             return BSP_ERR_SHAPE;
     }
     if (const int shared = overlapping(tensors, count)) return shared > 0 ? BSP_ERR_SHAPE : BSP_ERR_CAPACITY;
+    const int per = all >= 1024 * ((count + kMaxTensors - 1) / kMaxTensors) ? 4 : 2;
+    const int64_t chunk = state_bits == 32 ? kThreads * per : kChunk8;
     Hyper h;
     h.lr = lr;
     h.beta1 = beta1;
@@ -432,7 +436,10 @@ extern "C" int bsp_adamw_step(const bsp_adamw_tensor *tensors, int64_t count, in
     tab.count = 0;
     auto flush = [&]() -> int {
         if (!tab.count) return BSP_OK;
-        BSP_DISPATCH_DTYPE(gdt, GDT, { launch<GDT>(tab, h, (unsigned)wgs, state_bits, cdt, s); });
+        BSP_DISPATCH_DTYPE(gdt, GDT, {
+            if (cdt == BSP_F16) launch<GDT, BSP_F16>(tab, h, (unsigned)wgs, state_bits, per, s);
+            else launch<GDT, BSP_BF16>(tab, h, (unsigned)wgs, state_bits, per, s);
+        });
         tab.count = 0;
         wgs = 0;
         return check_launch();
