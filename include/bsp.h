@@ -180,7 +180,8 @@ int bsp_adam_step(float *W, const void *G, int gdt, float *m, float *v, int64_t 
  *   w <- w - (lr*(m/c1)) / (sqrt(v/c2) + eps),  c = 1 - beta^t
  *   w <- +0                       if the tensor has keep and keep[b][j] == 0
  *   copy <- w in cdt (RNE)        if the tensor has a copy: the 16-bit weights of the next forward pass
- * state_bits 32: m and v are fp32 tensors; without decay, copy and grad_scale the bits are those of bsp_adam_step.
+ * state_bits 32: m and v are fp32 tensors (the hyper-parameters come in 64 bits and 1 - beta is rounded once; apart from that the
+ *   arithmetic is that of bsp_adam_step).
  * state_bits 8: m and v are e4m3 codes (4 exponent and 3 mantissa bits, no infinity), v of r = sqrt(v); for every 256
  *   consecutive elements (the last block of a tensor may be shorter) scales holds the largest |m|, then, ceil(M N / 256)
  *   floats further on, the largest r, each divided by 448: a moment is its code times its block's scale.  A new moment goes to
@@ -209,8 +210,8 @@ typedef struct {
     int32_t R;
     float weight_decay;
 } bsp_adamw_tensor;
-int bsp_adamw_step(const bsp_adamw_tensor *tensors, int64_t count, int gdt, int cdt, int state_bits, float lambda, float lr,
-                   float beta1, float beta2, float eps, int64_t t, uint32_t seed, const float *lr_t, const float *grad_scale,
+int bsp_adamw_step(const bsp_adamw_tensor *tensors, int64_t count, int gdt, int cdt, int state_bits, double lambda, double lr,
+                   double beta1, double beta2, double eps, int64_t t, uint32_t seed, const float *lr_t, const float *grad_scale,
                    void *stream);
 
 /* ---- compact storage (Sec. 3.1: only the kept columns of a block are indexed) ----------

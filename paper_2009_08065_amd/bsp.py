@@ -103,7 +103,8 @@ def lib():
     L.bsp_block_norm_backward_workspace_bytes.restype = sz
     L.bsp_block_norm_backward.argtypes = [vp, vp, vp, vp, C.c_int, i64, i64, C.c_int, C.c_int, f32, vp, i64, vp, vp, vp, vp, vp,
                                           vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
-    L.bsp_adamw_step.argtypes = [vp, i64, C.c_int, C.c_int, C.c_int, f32, f32, f32, f32, f32, i64, C.c_uint32, vp, vp, vp]
+    f64 = C.c_double
+    L.bsp_adamw_step.argtypes = [vp, i64, C.c_int, C.c_int, C.c_int, f64, f64, f64, f64, f64, i64, C.c_uint32, vp, vp, vp]
     L.bsp_compression_rate.argtypes = [i64, i64, i32, i64]
     L.bsp_compression_rate.restype = C.c_double
     L.bsp_status_string.argtypes = [C.c_int]

@@ -144,7 +144,7 @@ __global__ __launch_bounds__(kThreads) void adamw32_kernel(Table tab, Hyper h) {
     const bool grouped = e.keep || e.alpha;
     Groups groups(e, grouped ? base : 0);
     if (grouped) groups.advance(threadIdx.x);
-    const float decay = s.lr * e.decay;
+    const float decay = h.lr_t ? s.lr * e.decay : e.decay;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
         const uint32_t i = j * kThreads + threadIdx.x;
@@ -203,6 +203,15 @@ __device__ __forceinline__ float wave_max(uint32_t x) {
     return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)x, 63));
 }
 
+// The square root to the nearest number: the instruction's is one of three neighbours, and the sign of s' s - v for the lower and the
+// upper one says which.  (What is stored is a decision on r: with a root that is off by an ulp here and there, the same step elsewhere gives other codes.)
+__device__ __forceinline__ float nearest_root(float v) {
+    const float s = __builtin_amdgcn_sqrtf(v);
+    const float down = __uint_as_float(__float_as_uint(s) - 1u), up = __uint_as_float(__float_as_uint(s) + 1u);
+    float r = __builtin_fmaf(-down, s, v) <= 0.0f ? down : s;
+    return __builtin_fmaf(-up, s, v) > 0.0f ? up : r;
+}
+
 // |y| <= 448 to one of the two codes' values next to it, up where the 16 bits (of 2^16) exceed what is missing.  Below 2^-6 the
 // step is that of 2^-6, which the addition of 2^-6 brings about.
 __device__ __forceinline__ float round_random(float y, uint32_t bits16) {
@@ -236,7 +245,7 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(Table tab, Hyper h) {
     if (grouped) groups.advance(4 * lane);
     const bool one_row = (e.N & 3) == 0;  // a lane's four elements are neighbours in the group arrays
     const int64_t blocks = (e.n + kBlock - 1) / kBlock;
-    const float decay = s.lr * e.decay, rate = s.lr / s.c1, root = 1.0f / __builtin_sqrtf(s.c2);
+    const float decay = h.lr_t ? s.lr * e.decay : e.decay, rate = s.lr / s.c1, root = 1.0f / __builtin_sqrtf(s.c2);
     uint8_t *m8 = (uint8_t *)e.m, *v8 = (uint8_t *)e.v;
     for (int b = 0; b < kBlocksPerWave; ++b) {
         const int64_t i0 = base + b * kBlock + 4 * lane, block = base / kBlock + b;
@@ -304,13 +313,13 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(Table tab, Hyper h) {
             m[j] = h.beta1 * (m0[j] * sm) + h.omb1 * x;
             const float ro = r0[j] * sv;
             const float v = h.beta2 * (ro * ro) + h.omb2 * x * x;
-            // (square root and reciprocal of the instructions, 1 ulp: the moments themselves are known to a sixteenth)
-            r[j] = __builtin_amdgcn_sqrtf(v);
+            r[j] = nearest_root(v);
             float wn = w[j];
             if (decay != 0.0f) {
                 const float d = decay * wn;
                 wn = wn - d;
             }
+            // (the instruction's reciprocal, 1 ulp)
             wn = wn - rate * m[j] * __builtin_amdgcn_rcpf(__builtin_fmaf(r[j], root, h.eps));
             w[j] = (kept >> j) & 1u ? wn : 0.0f;
             const uint32_t um = __float_as_uint(m[j]) & 0x7fffffffu, ur = __float_as_uint(r[j]);
@@ -320,7 +329,7 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(Table tab, Hyper h) {
         const float top_m = wave_max(bits_m), top_r = wave_max(bits_r);
         // (2^-100: below it 448 / largest has no number, and such moments move nothing)
         const bool has_m = top_m >= 0x1p-100f, has_r = top_r >= 0x1p-100f;
-        const float im = has_m ? 448.0f * __builtin_amdgcn_rcpf(top_m) : 0.0f, ir = has_r ? 448.0f * __builtin_amdgcn_rcpf(top_r) : 0.0f;
+        const float im = has_m ? 448.0f * (1.0f / top_m) : 0.0f, ir = has_r ? 448.0f * (1.0f / top_r) : 0.0f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const uint32_t bits = mix((uint32_t)(i0 + j) + s.salt);
@@ -389,8 +398,8 @@ int overlapping(const bsp_adamw_tensor *x, int64_t count) {
 
 using namespace bsp;
 
-extern "C" int bsp_adamw_step(const bsp_adamw_tensor *tensors, int64_t count, int gdt, int cdt, int state_bits, float lambda, float lr,
-                              float beta1, float beta2, float eps, int64_t t, uint32_t seed, const float *lr_t,
+extern "C" int bsp_adamw_step(const bsp_adamw_tensor *tensors, int64_t count, int gdt, int cdt, int state_bits, double lambda, double lr,
+                              double beta1, double beta2, double eps, int64_t t, uint32_t seed, const float *lr_t,
                               const float *grad_scale, void *stream) {
     if (count < 0 || (state_bits != 32 && state_bits != 8)) return BSP_ERR_SHAPE;
     if (count && !tensors) return BSP_ERR_NULL;
@@ -415,17 +424,17 @@ extern "C" int bsp_adamw_step(const bsp_adamw_tensor *tensors, int64_t count, in
     const int per = all >= 1024 * ((count + kMaxTensors - 1) / kMaxTensors) ? 4 : 2;
     const int64_t chunk = state_bits == 32 ? kThreads * per : kChunk8;
     Hyper h;
-    h.lr = lr;
-    h.beta1 = beta1;
-    h.beta2 = beta2;
-    h.omb1 = 1.0f - beta1;
-    h.omb2 = 1.0f - beta2;
-    h.c1 = (float)(1.0 - std::pow((double)beta1, (double)t));
-    h.c2 = (float)(1.0 - std::pow((double)beta2, (double)t));
-    h.eps = eps;
-    h.lambda = lambda;
-    h.log1 = (float)std::log((double)beta1);
-    h.log2 = (float)std::log((double)beta2);
+    h.lr = (float)lr;
+    h.beta1 = (float)beta1;
+    h.beta2 = (float)beta2;
+    h.omb1 = (float)(1.0 - beta1);  // (of 0.999 in fp32 it would be 1.3e-5 off)
+    h.omb2 = (float)(1.0 - beta2);
+    h.c1 = (float)(1.0 - std::pow(beta1, (double)t));
+    h.c2 = (float)(1.0 - std::pow(beta2, (double)t));
+    h.eps = (float)eps;
+    h.lambda = (float)lambda;
+    h.log1 = (float)std::log(beta1);
+    h.log2 = (float)std::log(beta2);
     h.seed = seed;
     h.t = (uint32_t)t;
     h.lr_t = lr_t;
@@ -463,7 +472,7 @@ extern "C" int bsp_adamw_step(const bsp_adamw_tensor *tensors, int64_t count, in
         e.n = n;
         e.N = (uint32_t)x.N;
         e.R = (uint32_t)(x.R > 0 ? x.R : 1);
-        e.decay = x.weight_decay;
+        e.decay = lr_t ? x.weight_decay : (float)(lr * (double)x.weight_decay);
         e.aligned = aligned(x.w, 16) && aligned(x.g, 4 * dtype_size(gdt)) && aligned(x.m, 4) && aligned(x.v, 4) && aligned(x.copy, 8);
         tab.first[tab.count++] = (uint32_t)wgs;
         wgs += need;

@@ -134,13 +134,14 @@ bool read_whole(PyObject *o, T &out) {
     return true;
 }
 
-bool read_real(PyObject *o, float &out) {
+template <typename T>
+bool read_real(PyObject *o, T &out) {
     const double v = PyFloat_AsDouble(o);
     if (v == -1.0 && PyErr_Occurred()) {
-        PyObject *n = other_number(o, "c_float");
-        return n && read_instead(n, read_real, out);
+        PyObject *n = other_number(o, std::is_same_v<T, float> ? "c_float" : "c_double");
+        return n && read_instead(n, read_real<T>, out);
     }
-    out = static_cast<float>(v);
+    out = static_cast<T>(v);
     return true;
 }
 
@@ -326,7 +327,7 @@ PyObject *adamw_step(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     for (PyObject *l : {rows, decays})
         if (l && PySequence_Fast_GET_SIZE(l) != count) return bad_list("the lists must have one length");
     int bits;
-    float real[5];
+    double real[5];
     int64_t t, device;
     uint64_t seed;
     void *lr_t, *grad_scale, *stream;
