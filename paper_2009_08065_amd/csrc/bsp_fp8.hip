@@ -15,7 +15,7 @@ namespace bsp {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPitch = 128 + 8;  // bytes of a column's codes in LDS: 8-byte writes of 16 threads fall into different banks
+constexpr int kPitch = 128 + 4;  // bytes of a column's codes in LDS
 
 struct Quant {
     const void *X;
@@ -79,42 +79,50 @@ __global__ __launch_bounds__(kThreads) void quant_rows_kernel(Quant a) {
     }
 }
 
+// The tile: kTileThreads threads of kEach rows x 8 columns each.  (With 8 x 8 values each, half the threads, the small matrices' chains of load,
+// largest value and store were twice as long: 8192 x 1024 in both orientations 13.5 us.)
+constexpr int kTileThreads = 512, kEach = 4, kTileWaves = kTileThreads / kWave;
+
 template <int DT, bool BLOCK, bool TRANSPOSED>
-__global__ __launch_bounds__(kThreads) void quant_kernel(Quant a) {
-    __shared__ float top[TRANSPOSED ? 4 * 128 : 4];
+__global__ __launch_bounds__(kTileThreads) void quant_kernel(Quant a) {
+    __shared__ float top[TRANSPOSED && !BLOCK ? kTileWaves * 128 : kTileWaves];
     __shared__ __align__(16) uint8_t turned[TRANSPOSED ? 128 * kPitch : 16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t tr = blockIdx.x / a.tiles_c, tc = blockIdx.x - tr * a.tiles_c;
-    const int r0 = 8 * (tid >> 4), c0 = 8 * (tid & 15);
+    const int r0 = kEach * (tid >> 4), c0 = 8 * (tid & 15);
     const int64_t row0 = 128 * tr + r0, col0 = 128 * tc + c0;
-    const int rows = a.rows - row0 > 8 ? 8 : (int)(a.rows - row0), cols = a.cols - col0 > 8 ? 8 : (int)(a.cols - col0);  // (may be negative)
+    const int rows = a.rows - row0 > kEach ? kEach : (int)(a.rows - row0), cols = a.cols - col0 > 8 ? 8 : (int)(a.cols - col0);  // (may be negative)
 
-    Piece<DT> v[8];
+    Piece<DT> v[kEach];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i].load(a.X, (row0 + i) * a.cols + col0, i < rows ? cols : 0);
+    for (int i = 0; i < kEach; ++i) v[i].load(a.X, (row0 + i) * a.cols + col0, i < rows ? cols : 0);
 
-    uint32_t e_row[8], e_col[8];  // biased exponents of the rows' and the columns' scales
+    uint32_t e_row[kEach], e_col[8];  // biased exponents of the rows' and the columns' scales
     if constexpr (BLOCK) {
         float m = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < kEach; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) m = __builtin_fmaxf(m, magnitude(v[i][j]));
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d));
+        m = max_of_16(m);
+        m = __builtin_fmaxf(m, __shfl_xor(m, 16));
+        m = __builtin_fmaxf(m, __shfl_xor(m, 32));
         if (lane == 0) top[wave] = m;
         __syncthreads();
-        m = __builtin_fmaxf(__builtin_fmaxf(top[0], top[1]), __builtin_fmaxf(top[2], top[3]));
+#pragma unroll
+        for (int w = 0; w < kTileWaves; ++w) m = __builtin_fmaxf(m, top[w]);
         const uint32_t e = scale_exponent(m);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e_row[i] = e_col[i] = e;
+        for (int i = 0; i < kEach; ++i) e_row[i] = e;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e_col[j] = e;
         if (tid == 0) {
             if (a.Q) a.S[tr * a.tiles_c + tc] = (uint8_t)e;
             if (TRANSPOSED) a.St[tc * (a.pitch_t / 128) + tr] = (uint8_t)e;
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < kEach; ++i) {
             float m = 0.0f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) m = __builtin_fmaxf(m, magnitude(v[i][j]));
@@ -127,24 +135,29 @@ __global__ __launch_bounds__(kThreads) void quant_kernel(Quant a) {
             for (int j = 0; j < 8; ++j) {
                 float m = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) m = __builtin_fmaxf(m, magnitude(v[i][j]));
+                for (int i = 0; i < kEach; ++i) m = __builtin_fmaxf(m, magnitude(v[i][j]));
                 m = __builtin_fmaxf(m, __shfl_xor(m, 16));
                 m = __builtin_fmaxf(m, __shfl_xor(m, 32));
                 if (lane < 16) top[wave * 128 + c0 + j] = m;
             }
             __syncthreads();
+            if (tid < 128) {  // a column's largest value, then its exponent in its place
+                float m = top[tid];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int c = c0 + j;
-                e_col[j] = scale_exponent(__builtin_fmaxf(__builtin_fmaxf(top[c], top[128 + c]), __builtin_fmaxf(top[256 + c], top[384 + c])));
-                if (tid < 16 && j < cols) a.St[(col0 + j) * (a.pitch_t / 128) + tr] = (uint8_t)e_col[j];
+                for (int w = 1; w < kTileWaves; ++w) m = __builtin_fmaxf(m, top[w * 128 + tid]);
+                const uint32_t e = scale_exponent(m);
+                top[tid] = __uint_as_float(e);
+                if (128 * tc + tid < a.cols) a.St[(128 * tc + tid) * (a.pitch_t / 128) + tr] = (uint8_t)e;
             }
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e_col[j] = __float_as_uint(top[c0 + j]);
         }
     }
 
     if (a.Q) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < kEach; ++i) {
             if (i >= rows) break;
             const float s = inverse_scale(e_row[i]);
             float y[8];
@@ -157,27 +170,28 @@ __global__ __launch_bounds__(kThreads) void quant_kernel(Quant a) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float s = inverse_scale(e_col[j]);
-            float y[8];
+            float y[kEach];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = s * v[i][j];
-            *reinterpret_cast<uint2 *>(turned + (c0 + j) * kPitch + r0) = make_uint2(codes4(y), codes4(y + 4));
+            for (int i = 0; i < kEach; ++i) y[i] = s * v[i][j];
+            *reinterpret_cast<uint32_t *>(turned + (c0 + j) * kPitch + r0) = codes4(y);
         }
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int c = (tid >> 4) + 16 * i;
-            if (128 * tc + c < a.cols)
-                *reinterpret_cast<uint2 *>(a.Qt + (128 * tc + c) * a.pitch_t + 128 * tr + 8 * (tid & 15)) =
-                    *reinterpret_cast<const uint2 *>(turned + c * kPitch + 8 * (tid & 15));
+        for (int n = tid; n < 128 * 8; n += kTileThreads) {
+            const int c = n >> 3, r = 16 * (n & 7);
+            if (128 * tc + c < a.cols) {
+                uint4 x;
+                __builtin_memcpy(&x, turned + c * kPitch + r, 16);
+                *reinterpret_cast<uint4 *>(a.Qt + (128 * tc + c) * a.pitch_t + 128 * tr + r) = x;
+            }
         }
     }
 }
 
 template <int DT>
 void launch(const Quant &a, unsigned grid, int64_t rows_grid, bool block, bool transposed, hipStream_t s) {
-    if (block && transposed) quant_kernel<DT, true, true><<<grid, kThreads, 0, s>>>(a);
-    else if (block) quant_kernel<DT, true, false><<<grid, kThreads, 0, s>>>(a);
-    else if (transposed) quant_kernel<DT, false, true><<<grid, kThreads, 0, s>>>(a);
+    if (block && transposed) quant_kernel<DT, true, true><<<grid, kTileThreads, 0, s>>>(a);
+    else if (block) quant_kernel<DT, true, false><<<grid, kTileThreads, 0, s>>>(a);
+    else if (transposed) quant_kernel<DT, false, true><<<grid, kTileThreads, 0, s>>>(a);
     else quant_rows_kernel<DT><<<(unsigned)rows_grid, kThreads, 0, s>>>(a);
 }
 

@@ -85,7 +85,7 @@ __global__ __launch_bounds__(64 * WA * WB) void fp8_tile_kernel(Product p) {
     }
     // and 64 rows' scales to a piece (in tiles of fewer pieces than wavefronts several load the same one)
     constexpr int kScalePieces = (TA + TB) / 64, kScaleLoads = (kScalePieces + kWaves - 1) / kWaves;
-    static_assert(TA % 64 == 0 && TB % 64 == 0 && (kScalePieces % kWaves == 0 || kScalePieces < kWaves));
+    static_assert(TA % 64 == 0 && TB % 64 == 0);
     const uint8_t *scale_base[kScaleLoads];
     uint32_t scale_at[kScaleLoads], scale_lds[kScaleLoads];
 #pragma unroll
@@ -455,7 +455,7 @@ double tile_us(int tile, double n, double steps, bool wide, bool gelu) {
     switch (tile) {
         case 256: return 5.0 + rounds * ((wide ? 3.2 : 1.62) * steps + 5.0 + (gelu ? 8.5 : 0.0));
         case 128: return 3.5 + pairs * ((wide ? 1.85 : 1.03) * steps + 2.2 + (gelu ? 2.5 : 0.0));
-        case 127: return 3.5 + rounds * ((wide ? 1.04 : 0.46) * steps + 1.5 + (gelu ? 2.5 : 0.0));
+        case 127: return 3.5 + rounds * ((wide ? 1.04 : n <= 256.0 ? 0.46 : 0.62) * steps + 1.5 + (gelu ? 2.5 : 0.0));
         case 64: return 3.5 + __builtin_ceil(n / 1024.0) * ((wide ? 1.25 : 0.83) * steps + 1.6 + (gelu ? 1.0 : 0.0));
         default:
             if (n <= 256.0) return 5.0 + (wide ? 0.41 : 0.215) * steps;
