@@ -194,9 +194,10 @@ int bsp_adam_step(float *W, const void *G, int gdt, float *m, float *v, int64_t 
  *   No two tensors of a call may overlap (weights that do, a tied tensor listed twice, are refused).  Addresses need
  *   their element's alignment.
  * lr_t: NULL, or two device floats {lr, t} that the kernels read in the place of the arguments: a step that was captured in
- *   a graph is replayed with new ones (t as a float: exact up to 2^24).
+ *   a graph is replayed with new ones (t as a float: exact up to 2^24).  A captured step without it repeats its t, and its random bits.
  * Up to 40 tensors are one launch.  Errors: BSP_ERR_NULL, BSP_ERR_DTYPE (gdt; cdt other than bf16 / fp16),
- * BSP_ERR_SHAPE (state_bits, t < 1 without lr_t, negative sizes, N >= 2^31, M % R != 0 with keep or alpha, misalignment,
+ * BSP_ERR_SHAPE (state_bits, t < 1 without lr_t, negative sizes, N >= 2^31, 2^34 elements or more, M % R != 0 with
+ * keep or alpha, misalignment,
  * weights that overlap), BSP_ERR_CAPACITY (no host memory for that check). */
 typedef struct {
     float *w;

@@ -633,22 +633,7 @@ def bsp_matmul_fp8(A: Fp8, B: Fp8, bias=None, act=0, residual=None, out_dtype=to
 
 def bsp_linear_fp8(X, W: Fp8, bias=None, act=0, residual=None, Y=None, ws=None):
     """The layer on X [T, N] with quantised weights [M, N]: X brought to 8 bits by rows, and bsp_matmul_fp8."""
-    native = _native()
-    _here(X, W.codes, W.scales, bias, residual, Y, ws)
-    T, N = X.shape
-    if N != W.cols:
-        raise ValueError("X has the wrong number of columns")
-    _fp8_fits(W)
-    if Y is None:
-        Y = native.empty(X, _DT[X.dtype], T, W.rows)
-    elif Y.dtype != X.dtype or tuple(Y.shape) != (T, W.rows):
-        raise ValueError("Y must be a [T, M] tensor of the dtype of X")
-    _epilogue_fits(T, W.rows, X.dtype, bias, residual)
-    if ws is None:
-        need = native.bsp_linear_fp8_workspace_bytes(T, W.rows, N)
-        ws = native.empty(X, _U8, need) if need else None
-    st = native.bsp_linear_fp8(X, _DT[X.dtype], T, W.rows, N, W.codes, W.scales, W.layout, bias, act, residual, Y, ws,
-                               0 if ws is None else ws.numel() * ws.element_size(), _stream())
+    st, Y = _native().linear_fp8(X, W.codes, W.scales, W.rows, W.cols, W.layout, bias, act, residual, Y, ws, torch._C._cuda_getDevice(), _stream())
     _check(st, "bsp_linear_fp8")
     return Y
 

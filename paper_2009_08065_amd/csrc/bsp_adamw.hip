@@ -25,6 +25,7 @@ constexpr int kThreads = 256;
 constexpr int kMaxTensors = 40;            // 40 entries of 88 bytes: a launch has 4 KB of arguments
 constexpr int kBlock = 256;                // elements of an 8-bit scale: one wavefront, 4 per lane
 constexpr int kBlocksPerWave = 4;
+constexpr int64_t kMostWorkgroups = (int64_t)1 << 24;  // of a launch, which has less than 2^32 threads
 constexpr int64_t kChunk8 = (kThreads / kWave) * kBlocksPerWave * kBlock;
 
 struct Entry {
@@ -414,7 +415,7 @@ extern "C" int bsp_adamw_step(const bsp_adamw_tensor *tensors, int64_t count, in
         if (!x.w || !x.g || !x.m || !x.v || (state_bits == 8 && !x.scales)) return BSP_ERR_NULL;
         if ((x.keep || x.alpha) && (x.R <= 0 || x.M % x.R != 0)) return BSP_ERR_SHAPE;
         const int64_t n = (x.M * x.N + largest - 1) / largest;
-        if (n >= ((int64_t)1 << 31)) return BSP_ERR_SHAPE;
+        if (n >= kMostWorkgroups) return BSP_ERR_SHAPE;
         all += n;
         if (!aligned(x.w, 4) || !aligned(x.g, dtype_size(gdt)) || (state_bits == 32 && (!aligned(x.m, 4) || !aligned(x.v, 4))) ||
             !aligned(x.scales, 4) || !aligned(x.copy, 2) || !aligned(x.alpha, 4))
@@ -458,7 +459,7 @@ extern "C" int bsp_adamw_step(const bsp_adamw_tensor *tensors, int64_t count, in
         const int64_t n = x.M * x.N;
         if (n == 0) continue;
         const int64_t need = (n + chunk - 1) / chunk;
-        if (tab.count == kMaxTensors || wgs + need >= ((int64_t)1 << 31))
+        if (tab.count == kMaxTensors || wgs + need >= kMostWorkgroups)
             if (int st = flush()) return st;
         Entry &e = tab.e[tab.count];
         e.w = x.w;

@@ -196,8 +196,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void block_norm_kernel(Forwa
     __shared__ float red[TPR > 64 ? 2 * (TPR / 64) : 1];
     int turn = 0;
     const int t = threadIdx.x % TPR, H = a.width;
-    const int64_t row = (int64_t)blockIdx.x * kTeams + threadIdx.x / TPR;
-    if (row >= a.T) return;  // (whole teams; a workgroup of one team has a row)
+    const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kTeams + threadIdx.x / TPR;
+    if (row >= a.T) return;  // (whole teams)
     const int64_t at = row * H;
     const bool post = a.F && (a.norms & BSP_NORM_POST), pre = (a.norms & BSP_NORM_PRE) != 0;
     // everything is asked for before the first sum is waited for
@@ -545,7 +545,8 @@ int check(int64_t T, int64_t H, int dt, int norms, int kind, const void *gate, i
 template <int DT, int TPR, int ITER>
 void launch_forward(const Forward &a, hipStream_t s) {
     constexpr int kTeams = TPR < 256 ? 256 / TPR : 1;
-    const unsigned grid = (unsigned)((a.T + kTeams - 1) / kTeams);
+    const int64_t wgs = (a.T + kTeams - 1) / kTeams, most = (int64_t)1 << 20;  // (a launch has less than 2^32 threads along x)
+    const dim3 grid((unsigned)(wgs < most ? wgs : most), (unsigned)((wgs + most - 1) / most));
     if (a.width % kVec == 0) block_norm_kernel<DT, TPR, ITER, true><<<grid, TPR < 256 ? 256 : TPR, 0, s>>>(a);
     else block_norm_kernel<DT, TPR, ITER, false><<<grid, TPR < 256 ? 256 : TPR, 0, s>>>(a);
 }

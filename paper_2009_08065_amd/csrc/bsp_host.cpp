@@ -413,10 +413,10 @@ PyObject *adamw_step(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     END_HANDLE_TH_ERRORS
 }
 
-// ---- the norms round a block ----------------------------------------------------------------------------------------------------
-// Checks, results and the call in one function: up to twelve tensors and seven results, which one by one from Python took 16 us for a backward
-// pass whose kernels take 9.
-struct NormArgs {
+// ---- calls with their checks and results ----------------------------------------------------------------------------------------------------
+// Checks, results and the call in one function.  One by one from Python the twelve tensors and seven results of a norm's backward pass took 16 us,
+// its kernels 9; a layer of one token in 8 bits 6.5, its kernel 4.
+struct RowArgs {
     const char *where;
     int64_t device;
     const at::Tensor *like = nullptr;
@@ -479,6 +479,49 @@ PyObject *with_status(int st, at::Tensor *results, int n) {
     return all;
 }
 
+// linear_fp8(X, codes, scales, rows, cols, layout, bias, act, residual, Y, ws, device, stream) -> (status, Y)
+PyObject *linear_fp8(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    if (n_args != 13) {
+        PyErr_Format(PyExc_TypeError, "this function takes 13 arguments (%zd given)", n_args);
+        return nullptr;
+    }
+    RowArgs a{"bsp_linear_fp8", 0};
+    const at::Tensor *X, *codes, *scales, *bias, *residual, *Y, *ws;
+    int64_t M, N;
+    int layout, act;
+    if (!read_whole(args[11], a.device) || !a.rows(args[0], X)) return nullptr;
+    if (!X) return a.fail("X must be a tensor"), nullptr;
+    if (!a.take(args[1], codes) || !a.take(args[2], scales) || !read_whole(args[3], M) || !read_whole(args[4], N) || !read_whole(args[5], layout) ||
+        !a.take(args[6], bias) || !read_whole(args[7], act) || !a.take(args[8], residual) || !a.take(args[9], Y) || !a.take(args[10], ws))
+        return nullptr;
+    void *stream = PyLong_AsVoidPtr(args[12]);
+    if (PyErr_Occurred()) return nullptr;
+    const int64_t T = X->size(0), steps = (N + 127) / 128, lines = layout == BSP_FP8_BLOCK ? (M + 127) / 128 : M;
+    if (X->size(1) != N) return a.fail("X has the wrong number of columns"), nullptr;
+    if (!codes || !scales || codes->scalar_type() != at::kFloat8_e4m3fn || codes->numel() != M * steps * 128 || scales->scalar_type() != at::kByte ||
+        scales->numel() != lines * steps)
+        return a.fail("codes (float8_e4m3fn) and scales (uint8) do not have the sizes of their matrix"), nullptr;
+    const at::ScalarType type = X->scalar_type();
+    if (bias && (bias->scalar_type() != type || bias->numel() != M)) return a.fail("bias must have M elements of the dtype of X"), nullptr;
+    for (const at::Tensor *t : {residual, Y})
+        if (t && (t->scalar_type() != type || t->dim() != 2 || t->size(0) != T || t->size(1) != M))
+            return a.fail("residual and Y must be [T, M] tensors of the dtype of X"), nullptr;
+    at::Tensor out;
+    int st;
+    {
+        const Unlocked unlocked;
+        out = Y ? *Y : a.make({T, M}, type);
+        at::Tensor scratch;
+        size_t bytes = ws ? (size_t)ws->nbytes() : bsp_linear_fp8_workspace_bytes(T, M, N);
+        if (!ws && bytes) scratch = a.make({(int64_t)bytes}, at::kByte);
+        st = bsp_linear_fp8(X->data_ptr(), a.type(), T, M, N, codes->data_ptr(), (const uint8_t *)scales->data_ptr(), layout, address(bias), act,
+                            address(residual), out.data_ptr(), ws ? ws->data_ptr() : (bytes ? scratch.data_ptr() : nullptr), bytes, stream);
+    }
+    return with_status(st, &out, 1);
+    END_HANDLE_TH_ERRORS
+}
+
 enum NormWant : unsigned { kWantZ = 1, kWantStatsPost = 2, kWantStatsPre = 4 };
 
 // block_norm(X, F, norms, kind, eps, x_scale, gate, w_post, b_post, w_pre, b_pre, Z, H, want, device, stream) -> (status, Z, H, stats_post, stats_pre)
@@ -488,7 +531,7 @@ PyObject *block_norm(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
         PyErr_Format(PyExc_TypeError, "this function takes 16 arguments (%zd given)", n_args);
         return nullptr;
     }
-    NormArgs a{"bsp_block_norm", 0};
+    RowArgs a{"bsp_block_norm", 0};
     const at::Tensor *X, *F, *gate, *w[4], *Z, *H;
     int norms, kind;
     float eps, x_scale;
@@ -531,7 +574,7 @@ PyObject *block_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n_ar
         PyErr_Format(PyExc_TypeError, "this function takes 20 arguments (%zd given)", n_args);
         return nullptr;
     }
-    NormArgs a{"bsp_block_norm_backward", 0};
+    RowArgs a{"bsp_block_norm_backward", 0};
     const at::Tensor *dZ, *dH, *Z, *F, *gate, *w[4], *sp, *sq, *dX, *dF, *ws;
     int norms, kind;
     float x_scale;
@@ -605,8 +648,7 @@ PyMethodDef methods[] = {
     BSP_ENTRY(bsp_fp8_quant, kByte),
     BSP_ENTRY(bsp_matmul_fp8_workspace_bytes, kNone),
     BSP_ENTRY(bsp_matmul_fp8, kByte),
-    BSP_ENTRY(bsp_linear_fp8_workspace_bytes, kNone),
-    BSP_ENTRY(bsp_linear_fp8, kByte),
+    {"linear_fp8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&linear_fp8)), METH_FASTCALL, nullptr},
     {"block_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&block_norm)), METH_FASTCALL, nullptr},
     {"block_norm_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&block_norm_backward)), METH_FASTCALL, nullptr},
     {"bsp_adamw_step", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&adamw_step)), METH_FASTCALL, nullptr},

@@ -128,10 +128,10 @@ def block_norm_backward(dz, dh, z, f, post, pre, rms, x_scale, gate, w_post, b_p
 
 
 # ---- AdamW --------------------------------------------------------------------------------------------------------------------
-def random_bits(n, t, seed):
-    """(16 bits for m, 16 bits for r) of the elements 0 .. n - 1."""
+def random_bits(n, t, seed, first=0):
+    """(16 bits for m, 16 bits for r) of the elements first .. first + n - 1."""
     low = 0xFFFFFFFF
-    x = (torch.arange(n) + ((seed * 0x9E3779B1 + t * 0x6A09E667) & low)) & low
+    x = (torch.arange(first, first + n) + ((seed * 0x9E3779B1 + t * 0x6A09E667) & low)) & low
     x = ((x ^ (x >> 16)) * 0xBB67AE85) & low
     x = ((x ^ (x >> 15)) * 0x3C6EF373) & low
     x = x ^ (x >> 16)

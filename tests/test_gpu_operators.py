@@ -534,6 +534,91 @@ def test_adamw_refuses_what_does_not_fit():
     assert not w.any()
 
 
+def test_products_and_norms_refuse_what_does_not_fit():
+    x = torch.zeros(40, 128, dtype=torch.bfloat16, device="cuda")
+    W = bsp.bsp_fp8_quant(torch.zeros(64, 128, device="cuda"), bsp.FP8_BLOCK)[0]
+    A = bsp.bsp_fp8_quant(x)[0]
+    row = lambda **k: bsp.Fp8(**{**dict(codes=W.codes, scales=W.scales, rows=64, cols=128, layout=bsp.FP8_BLOCK), **k})  # noqa: E731
+    half, one = torch.zeros(64, dtype=torch.float16, device="cuda"), torch.zeros(64, dtype=torch.bfloat16, device="cuda")
+    for call in (lambda: bsp.bsp_linear_fp8(x[:, :64].contiguous(), W), lambda: bsp.bsp_linear_fp8(x.cpu(), W), lambda: bsp.bsp_linear_fp8(x.t(), W),
+                 lambda: bsp.bsp_linear_fp8(x.double(), W), lambda: bsp.bsp_linear_fp8(x, row(rows=65)), lambda: bsp.bsp_linear_fp8(x, row(layout=bsp.FP8_ROW)),
+                 lambda: bsp.bsp_linear_fp8(x, row(codes=W.codes.view(torch.uint8))), lambda: bsp.bsp_linear_fp8(x, row(scales=W.scales.float())),
+                 lambda: bsp.bsp_linear_fp8(x, W, half), lambda: bsp.bsp_linear_fp8(x, W, one[:63]), lambda: bsp.bsp_linear_fp8(x, W, residual=x),
+                 lambda: bsp.bsp_linear_fp8(x, W, Y=x), lambda: bsp.bsp_matmul_fp8(row(), row()), lambda: bsp.bsp_matmul_fp8(A, row(cols=256)),
+                 lambda: bsp.bsp_matmul_fp8(A, W, half), lambda: bsp.bsp_matmul_fp8(A, W, residual=x), lambda: bsp.bsp_matmul_fp8(A, W, Y=x),
+                 lambda: bsp.bsp_fp8_quant(x.t()), lambda: bsp.bsp_fp8_quant(x.cpu()),
+                 lambda: bsp.bsp_block_norm(x, x[:20]), lambda: bsp.bsp_block_norm(x, x.float()), lambda: bsp.bsp_block_norm(x, w_pre=one),
+                 lambda: bsp.bsp_block_norm(x, x, gate=half.view(1, 64)), lambda: bsp.bsp_block_norm(x.cpu()), lambda: bsp.bsp_block_norm(x.double()),
+                 lambda: bsp.bsp_block_norm(x[0]), lambda: bsp.bsp_block_norm_backward(None, None, x), lambda: bsp.bsp_block_norm_backward(x, x[:20], x),
+                 lambda: bsp.bsp_block_norm_backward(x, x, x, stats_pre=torch.zeros(40, device="cuda")), lambda: bsp.bsp_block_norm(x, x, dX=x)):
+        with pytest.raises((ValueError, TypeError)):
+            call()
+    for call in (lambda: bsp.bsp_block_norm(x, x, norms=0), lambda: bsp.bsp_block_norm(x, norms=bsp.NORM_POST), lambda: bsp.bsp_block_norm(x, kind=3),
+                 lambda: bsp.bsp_block_norm(x, x, gate=torch.zeros(3, 128, dtype=x.dtype, device="cuda")), lambda: bsp.bsp_block_norm_backward(x, x, x),
+                 lambda: bsp.bsp_linear_fp8(x, W, act=5), lambda: bsp.bsp_block_norm(torch.zeros(2, 8200, device="cuda")),
+                 lambda: bsp.bsp_linear_fp8(x, W, ws=torch.zeros(256, dtype=torch.uint8, device="cuda"))):
+        with pytest.raises(bsp.BspError):
+            call()
+
+
+# ---- sizes past 32 bits -------------------------------------------------------------------------------------------------------
+def test_products_past_32_bits():
+    """More than 2^31 elements of X: the last rows are those of a call of their own."""
+    T, M, N = (1 << 21) + 37, 80, 1100
+    x = torch.zeros(T, N, dtype=torch.bfloat16, device="cuda")
+    x[-300:] = rand(1, 300, N, dt=torch.bfloat16).cuda()
+    W = bsp.bsp_fp8_quant(rand(2, M, N).cuda(), bsp.FP8_BLOCK)[0]
+    y = bsp.bsp_linear_fp8(x, W)
+    assert not y[:-300].any()
+    tail = bsp.bsp_matmul_fp8(bsp.bsp_fp8_quant(x[-300:].clone())[0], W, out_dtype=torch.float32)
+    assert float((y[-300:].float() - tail).norm() / tail.norm()) <= 2.0 ** -8 + 2.0 ** -13
+
+
+def test_norms_past_32_bits_and_past_one_row_of_workgroups():
+    T, H = (1 << 18) + 5, 8192
+    x = torch.zeros(T, H, dtype=torch.bfloat16, device="cuda")
+    x[-9:] = rand(1, 9, H, dt=torch.bfloat16).cuda()
+    h = bsp.bsp_block_norm(x, want=())[1]
+    assert torch.equal(h[-9:], bsp.bsp_block_norm(x[-9:].clone(), want=())[1]) and not h[:-9].any()
+    del h
+    st = bsp.bsp_block_norm(x, want=("stats_pre",))[3]
+    out = bsp.bsp_block_norm_backward(None, x, x, stats_pre=st, want=("dx",))
+    small = bsp.bsp_block_norm_backward(None, x[-9:].clone(), x[-9:].clone(), stats_pre=st[-9:].clone(), want=("dx",))
+    assert torch.equal(out["dx"][-9:], small["dx"])
+    del x, out
+    T = (1 << 22) + 4099                                # more than 2^20 workgroups
+    x = rand(2, T, 8).cuda()
+    h = bsp.bsp_block_norm(x, eps=1e-5)[1]
+    for part in (slice(0, 5000), slice(T - 5000, T)):
+        assert torch.equal(h[part], bsp.bsp_block_norm(x[part].clone(), eps=1e-5)[1])
+
+
+def test_adamw_past_32_bits():
+    M, N = (1 << 21) + 32, 1024
+    w = torch.zeros(M, N, device="cuda")
+    g = torch.zeros(M, N, dtype=torch.bfloat16, device="cuda")
+    keep = torch.ones(M // 16, N, dtype=torch.uint8, device="cuda")
+    w[-48:], g[-48:] = rand(1, 48, N).cuda(), rand(2, 48, N, dt=torch.bfloat16).cuda()
+    keep[-3:] = (rand(3, 3, N) > 0).to(torch.uint8).cuda()
+    tail = [t[-48:].clone() for t in (w, g)]
+    m, v, _ = bsp.bsp_adamw_state([w])
+    bsp.bsp_adamw_step([w], [g], m, v, 1e-2, keep=[keep], **HYPER)
+    m1, v1, _ = bsp.bsp_adamw_state([tail[0]])
+    bsp.bsp_adamw_step([tail[0]], [tail[1]], m1, v1, 1e-2, keep=[keep[-3:].clone()], **HYPER)
+    assert torch.equal(w[-48:], tail[0]) and torch.equal(m[0][-48:], m1[0]) and torch.equal(v[0][-48:], v1[0])
+    del m, v
+    w[-48:] = rand(1, 48, N).cuda()
+    m, v, s = bsp.bsp_adamw_state([w], 8)
+    bsp.bsp_adamw_step([w], [g], m, v, 1e-2, keep=[keep], scales=s, seed=4, **HYPER)
+    assert float((w[-48:] - tail[0]).abs().max()) <= 1e-2 * 24 * U + 4 * U * 5   # as above, |update| <= lr, |w| < 5
+    x = 0.1 * g[-1].cpu().to(D)                          # m of the last row, whose places are past 2^31
+    place = (M - 1) * N
+    bits = orc.random_bits(N, 1, 4, first=place)[0]
+    q, scale, near = orc.stored(x, bits, False)
+    got = orc.from_codes(m[0][-1].view(torch.uint8).cpu())
+    assert not ((got != q) & (near > 1e-4)).any() and float((s[0][0, -4:].cpu().to(D) / scale - 1).abs().max()) <= 12 * U
+
+
 # ---- together -----------------------------------------------------------------------------------------------------------------
 def encoder_block(x, w, b, gate, w_pre, b_pre, w_post, dz, state=None):
     """Norm, 8-bit layer, norm, gate and addition; gradients; an AdamW step of all its parameters (fp32 masters with 16-bit copies)."""
