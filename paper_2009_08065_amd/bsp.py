@@ -21,7 +21,7 @@ _TORCH = {F32: torch.float32, BF16: torch.bfloat16, F16: torch.float16}
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
 _NATIVE = None
-_U8, _I32, _E4M3 = 3, 4, 5  # types of a native allocation that are none of the library's
+_U8, _I32 = 3, 4  # types of a native allocation that are none of the library's
 
 
 class BspError(RuntimeError):
@@ -148,14 +148,6 @@ def _stream():
     """The current stream of the current device as an integer.  (torch.cuda.current_stream() builds a Stream object for
     it: 2.8 of the 9.9 us that a call of bsp_linear_planned took on the host; this takes 0.1.)"""
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
-
-
-def _here(*tensors):
-    """The kernels go to the current device's stream: tensors of another one are refused."""
-    device = torch._C._cuda_getDevice()
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise ValueError(f"tensors must be on the current device ({device}), got one on {t.device}")
 
 
 def _scratch(need: int, device):
@@ -576,57 +568,18 @@ class Fp8:
     layout: int
 
 
-def _fp8_fits(q: Fp8):
-    steps = (q.cols + 127) // 128
-    lines = q.rows if q.layout == FP8_ROW else (q.rows + 127) // 128
-    if q.codes.dtype != torch.float8_e4m3fn or q.codes.numel() != q.rows * steps * 128 or q.scales.numel() != lines * steps:
-        raise ValueError("codes (float8_e4m3fn) and scales do not have the sizes of their matrix")
-
-
 def bsp_fp8_quant(X, layout=FP8_ROW, want=("plain",)):
     """X [rows, cols] in 8 bits: (Fp8 of X, Fp8 of the transposed X), the ones not in `want` ("plain", "transposed") None."""
-    native = _native()
-    _here(X)
-    rows, cols = X.shape
-    made = []
-    for name, r, c in (("plain", rows, cols), ("transposed", cols, rows)):
-        if name not in want:
-            made.append(None)
-            continue
-        steps = (c + 127) // 128
-        lines = r if layout == FP8_ROW else (r + 127) // 128
-        made.append(Fp8(native.empty(X, _E4M3, r, steps * 128), native.empty(X, _U8, lines, steps), r, c, layout))
-    p, t = made
-    st = native.bsp_fp8_quant(X, _DT[X.dtype], rows, cols, layout, p and p.codes, p and p.scales, t and t.codes, t and t.scales, _stream())
+    st, Q, S, Qt, St = _native().fp8_quant(X, layout, ("plain" in want) | ("transposed" in want) << 1, torch._C._cuda_getDevice(), _stream())
     _check(st, "bsp_fp8_quant")
-    return p, t
-
-
-def _epilogue_fits(T, M, dtype, bias, residual):
-    if bias is not None and (bias.dtype != dtype or bias.numel() != M):
-        raise ValueError("bias must have M elements of the dtype of the result")
-    if residual is not None and (residual.dtype != dtype or tuple(residual.shape) != (T, M)):
-        raise ValueError("residual must be a [T, M] tensor of the dtype of the result")
+    rows, cols = X.shape
+    return (None if Q is None else Fp8(Q, S, rows, cols, layout)), (None if Qt is None else Fp8(Qt, St, cols, rows, layout))
 
 
 def bsp_matmul_fp8(A: Fp8, B: Fp8, bias=None, act=0, residual=None, out_dtype=torch.bfloat16, Y=None):
     """Y = round(act(A B^T + bias) + residual) of quantised A [T, K] (FP8_ROW) and B [M, K]."""
-    native = _native()
-    _here(A.codes, A.scales, B.codes, B.scales, bias, residual, Y)
-    T, M, K = A.rows, B.rows, A.cols
-    if A.layout != FP8_ROW or B.cols != K:
-        raise ValueError("A must be quantised by rows and have the columns of B")
-    _fp8_fits(A)
-    _fp8_fits(B)
-    if Y is None:
-        Y = native.empty(A.codes, _DT[out_dtype], T, M)
-    elif tuple(Y.shape) != (T, M):
-        raise ValueError("Y must be [T, M]")
-    _epilogue_fits(T, M, Y.dtype, bias, residual)
-    need = native.bsp_matmul_fp8_workspace_bytes(T, M, K)
-    ws = _scratch(need, Y.device)
-    st = native.bsp_matmul_fp8(A.codes, A.scales, B.codes, B.scales, B.layout, T, M, K, bias, act, residual, Y, _DT[Y.dtype], ws,
-                               0 if ws is None else need, _stream())
+    st, Y = _native().matmul_fp8(A.codes, A.scales, A.rows, A.cols, A.layout, B.codes, B.scales, B.rows, B.cols, B.layout, bias, act, residual,
+                                 _DT[out_dtype if Y is None else Y.dtype], Y, torch._C._cuda_getDevice(), _stream())
     _check(st, "bsp_matmul_fp8")
     return Y
 

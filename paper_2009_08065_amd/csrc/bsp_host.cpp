@@ -221,20 +221,20 @@ PyObject *empty_beside_other(PyObject *like, const char *type, const int64_t *si
     return result;
 }
 
-// empty(like, type, n) or empty(like, type, n, m): a tensor on the device of `like`; type: a bsp_dtype, 3 uint8, 4 int32, 5 float8_e4m3fn.
+// empty(like, type, n) or empty(like, type, n, m): a tensor on the device of `like`; type: a bsp_dtype, 3 uint8, 4 int32.
 PyObject *empty(PyObject *, PyObject *const *args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     if (n != 3 && n != 4) {
         PyErr_SetString(PyExc_TypeError, "empty(tensor, type, n[, m])");
         return nullptr;
     }
-    constexpr at::ScalarType types[] = {at::kFloat, at::kBFloat16, at::kHalf, at::kByte, at::kInt, at::kFloat8_e4m3fn};
-    constexpr const char *names[] = {"float32", "bfloat16", "float16", "uint8", "int32", "float8_e4m3fn"};
+    constexpr at::ScalarType types[] = {at::kFloat, at::kBFloat16, at::kHalf, at::kByte, at::kInt};
+    constexpr const char *names[] = {"float32", "bfloat16", "float16", "uint8", "int32"};
     const long long type = PyLong_AsLongLong(args[1]);
     int64_t size[2] = {0, 0};
     for (Py_ssize_t i = 2; i < n; ++i) size[i - 2] = PyLong_AsLongLong(args[i]);
     if (PyErr_Occurred()) return nullptr;
-    if (type < 0 || type > 5) {
+    if (type < 0 || type > 4) {
         PyErr_SetString(PyExc_ValueError, "unknown type");
         return nullptr;
     }
@@ -479,6 +479,97 @@ PyObject *with_status(int st, at::Tensor *results, int n) {
     return all;
 }
 
+// A quantised matrix [rows, cols] given as codes and scales.
+struct Coded {
+    const at::Tensor *codes, *scales;
+    int64_t rows, cols;
+    int layout;
+    // args: codes, scales, rows, cols, layout
+    bool read(const RowArgs &a, PyObject *const *args) {
+        if (!a.take(args[0], codes) || !a.take(args[1], scales) || !read_whole(args[2], rows) || !read_whole(args[3], cols) || !read_whole(args[4], layout))
+            return false;
+        const int64_t steps = (cols + 127) / 128, lines = layout == BSP_FP8_BLOCK ? (rows + 127) / 128 : rows;
+        return codes && scales && rows >= 0 && cols > 0 && codes->scalar_type() == at::kFloat8_e4m3fn && codes->numel() == rows * steps * 128 &&
+                       scales->scalar_type() == at::kByte && scales->numel() == lines * steps
+                   ? true
+                   : a.fail("codes (float8_e4m3fn) and scales (uint8) do not have the sizes of their matrix");
+    }
+};
+
+// fp8_quant(X, layout, want, device, stream) -> (status, Q, S, Qt, St); want: 1 for X, 2 for the transposed X
+PyObject *fp8_quant(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    if (n_args != 5) {
+        PyErr_Format(PyExc_TypeError, "this function takes 5 arguments (%zd given)", n_args);
+        return nullptr;
+    }
+    RowArgs a{"bsp_fp8_quant", 0};
+    const at::Tensor *X;
+    int layout;
+    uint32_t want;
+    if (!read_whole(args[3], a.device) || !a.rows(args[0], X)) return nullptr;
+    if (!X) return a.fail("X must be a tensor"), nullptr;
+    if (!read_whole(args[1], layout) || !read_whole(args[2], want)) return nullptr;
+    void *stream = PyLong_AsVoidPtr(args[4]);
+    if (PyErr_Occurred()) return nullptr;
+    at::Tensor out[4];
+    int st;
+    {
+        const Unlocked unlocked;
+        const int64_t rows = X->size(0), cols = X->size(1);
+        for (int i = 0; i < 2; ++i)
+            if ((want >> i) & 1u) {
+                const int64_t r = i ? cols : rows, steps = ((i ? rows : cols) + 127) / 128;
+                out[2 * i] = a.make({r, 128 * steps}, at::kFloat8_e4m3fn);
+                out[2 * i + 1] = a.make({layout == BSP_FP8_BLOCK ? (r + 127) / 128 : r, steps}, at::kByte);
+            }
+        auto at_of = [](at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
+        st = bsp_fp8_quant(X->data_ptr(), a.type(), rows, cols, layout, at_of(out[0]), (uint8_t *)at_of(out[1]), at_of(out[2]), (uint8_t *)at_of(out[3]), stream);
+    }
+    return with_status(st, out, 4);
+    END_HANDLE_TH_ERRORS
+}
+
+// matmul_fp8(A's codes, scales, rows, cols, layout, B's, bias, act, residual, type, Y, device, stream) -> (status, Y); type: a bsp_dtype, of Y where that is None
+PyObject *matmul_fp8(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    if (n_args != 17) {
+        PyErr_Format(PyExc_TypeError, "this function takes 17 arguments (%zd given)", n_args);
+        return nullptr;
+    }
+    RowArgs a{"bsp_matmul_fp8", 0};
+    Coded A, B;
+    const at::Tensor *bias, *residual, *Y;
+    int act, type;
+    if (!read_whole(args[15], a.device) || !A.read(a, args) || !B.read(a, args + 5) || !a.take(args[10], bias) || !read_whole(args[11], act) ||
+        !a.take(args[12], residual) || !read_whole(args[13], type) || !a.take(args[14], Y))
+        return nullptr;
+    void *stream = PyLong_AsVoidPtr(args[16]);
+    if (PyErr_Occurred()) return nullptr;
+    if (A.layout != BSP_FP8_ROW || A.cols != B.cols) return a.fail("A must be quantised by rows and have the columns of B"), nullptr;
+    constexpr at::ScalarType types[] = {at::kFloat, at::kBFloat16, at::kHalf};
+    if (type < 0 || type > 2) return a.fail("unknown type"), nullptr;
+    const int64_t T = A.rows, M = B.rows, K = A.cols;
+    if (bias && (bias->scalar_type() != types[type] || bias->numel() != M)) return a.fail("bias must have M elements of the dtype of the result"), nullptr;
+    for (const at::Tensor *t : {residual, Y})
+        if (t && (t->scalar_type() != types[type] || t->dim() != 2 || t->size(0) != T || t->size(1) != M))
+            return a.fail("residual and Y must be [T, M] tensors of the dtype of the result"), nullptr;
+    a.like = A.codes;
+    at::Tensor out;
+    int st;
+    {
+        const Unlocked unlocked;
+        out = Y ? *Y : a.make({T, M}, types[type]);
+        at::Tensor scratch;
+        size_t bytes = bsp_matmul_fp8_workspace_bytes(T, M, K);
+        if (bytes) scratch = a.make({(int64_t)bytes}, at::kByte);
+        st = bsp_matmul_fp8(A.codes->data_ptr(), (const uint8_t *)A.scales->data_ptr(), B.codes->data_ptr(), (const uint8_t *)B.scales->data_ptr(), B.layout,
+                            T, M, K, address(bias), act, address(residual), out.data_ptr(), type, bytes ? scratch.data_ptr() : nullptr, bytes, stream);
+    }
+    return with_status(st, &out, 1);
+    END_HANDLE_TH_ERRORS
+}
+
 // linear_fp8(X, codes, scales, rows, cols, layout, bias, act, residual, Y, ws, device, stream) -> (status, Y)
 PyObject *linear_fp8(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     HANDLE_TH_ERRORS
@@ -487,21 +578,18 @@ PyObject *linear_fp8(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
         return nullptr;
     }
     RowArgs a{"bsp_linear_fp8", 0};
-    const at::Tensor *X, *codes, *scales, *bias, *residual, *Y, *ws;
-    int64_t M, N;
-    int layout, act;
+    const at::Tensor *X, *bias, *residual, *Y, *ws;
+    Coded W;
+    int act;
     if (!read_whole(args[11], a.device) || !a.rows(args[0], X)) return nullptr;
     if (!X) return a.fail("X must be a tensor"), nullptr;
-    if (!a.take(args[1], codes) || !a.take(args[2], scales) || !read_whole(args[3], M) || !read_whole(args[4], N) || !read_whole(args[5], layout) ||
-        !a.take(args[6], bias) || !read_whole(args[7], act) || !a.take(args[8], residual) || !a.take(args[9], Y) || !a.take(args[10], ws))
+    if (!W.read(a, args + 1) || !a.take(args[6], bias) || !read_whole(args[7], act) || !a.take(args[8], residual) || !a.take(args[9], Y) ||
+        !a.take(args[10], ws))
         return nullptr;
     void *stream = PyLong_AsVoidPtr(args[12]);
     if (PyErr_Occurred()) return nullptr;
-    const int64_t T = X->size(0), steps = (N + 127) / 128, lines = layout == BSP_FP8_BLOCK ? (M + 127) / 128 : M;
+    const int64_t T = X->size(0), M = W.rows, N = W.cols;
     if (X->size(1) != N) return a.fail("X has the wrong number of columns"), nullptr;
-    if (!codes || !scales || codes->scalar_type() != at::kFloat8_e4m3fn || codes->numel() != M * steps * 128 || scales->scalar_type() != at::kByte ||
-        scales->numel() != lines * steps)
-        return a.fail("codes (float8_e4m3fn) and scales (uint8) do not have the sizes of their matrix"), nullptr;
     const at::ScalarType type = X->scalar_type();
     if (bias && (bias->scalar_type() != type || bias->numel() != M)) return a.fail("bias must have M elements of the dtype of X"), nullptr;
     for (const at::Tensor *t : {residual, Y})
@@ -515,7 +603,7 @@ PyObject *linear_fp8(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
         at::Tensor scratch;
         size_t bytes = ws ? (size_t)ws->nbytes() : bsp_linear_fp8_workspace_bytes(T, M, N);
         if (!ws && bytes) scratch = a.make({(int64_t)bytes}, at::kByte);
-        st = bsp_linear_fp8(X->data_ptr(), a.type(), T, M, N, codes->data_ptr(), (const uint8_t *)scales->data_ptr(), layout, address(bias), act,
+        st = bsp_linear_fp8(X->data_ptr(), a.type(), T, M, N, W.codes->data_ptr(), (const uint8_t *)W.scales->data_ptr(), W.layout, address(bias), act,
                             address(residual), out.data_ptr(), ws ? ws->data_ptr() : (bytes ? scratch.data_ptr() : nullptr), bytes, stream);
     }
     return with_status(st, &out, 1);
@@ -645,9 +733,8 @@ PyMethodDef methods[] = {
     BSP_ENTRY(bsp_linear_plan, kNone),
     BSP_ENTRY(bsp_linear_planned, kNone),
     BSP_ENTRY(bsp_linear_planned_fused, kNone),
-    BSP_ENTRY(bsp_fp8_quant, kByte),
-    BSP_ENTRY(bsp_matmul_fp8_workspace_bytes, kNone),
-    BSP_ENTRY(bsp_matmul_fp8, kByte),
+    {"fp8_quant", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&fp8_quant)), METH_FASTCALL, nullptr},
+    {"matmul_fp8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&matmul_fp8)), METH_FASTCALL, nullptr},
     {"linear_fp8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&linear_fp8)), METH_FASTCALL, nullptr},
     {"block_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&block_norm)), METH_FASTCALL, nullptr},
     {"block_norm_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&block_norm_backward)), METH_FASTCALL, nullptr},
