@@ -97,15 +97,17 @@ __global__ __launch_bounds__(64 * WA * WB) void fp8_tile_kernel(Product p) {
         scale_at[i] = (uint32_t)(blocks ? (m0 + row) / 128 - m0 / 128 : row) * (uint32_t)p.steps;
         scale_lds[i] = (uint32_t)(kCodes + piece * 256);
     }
-    auto load = [&](int step, int slot) {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
+    constexpr int kEach = kLoads + kScaleLoads;  // loads of a wavefront and step
+    auto load_one = [&](auto which, int step, int slot) {
+        constexpr int i = decltype(which)::value;
+        if constexpr (i < kLoads) {
             const int r8 = wave * kLoads + i, op = 8 * r8 >= TA;
             load_to_lds(slot * kStage + r8 * 1024, base[op] + (int64_t)step * 128, at[i]);
+        } else {
+            load_bytes_to_lds(slot * kStage + scale_lds[i - kLoads], scale_base[i - kLoads] + step, scale_at[i - kLoads]);
         }
-#pragma unroll
-        for (int i = 0; i < kScaleLoads; ++i) load_bytes_to_lds(slot * kStage + scale_lds[i], scale_base[i] + step, scale_at[i]);
     };
+    auto load = [&](int step, int slot) { static_for<0, kEach>([&](auto i) { load_one(i, step, slot); }); };
     f32x16 acc[FA][FB];
 #pragma unroll
     for (int i = 0; i < FA; ++i)
@@ -145,7 +147,10 @@ __global__ __launch_bounds__(64 * WA * WB) void fp8_tile_kernel(Product p) {
 #pragma unroll
         for (int j = 0; j < FB; ++j) o.b[j] = operand(cell_b, slot, j, sub);
     };
-    auto multiply = [&](const Operands &o) {
+    // The products of half a step; after each of them `between` may put something else: what is issued in a row (a wavefront's loads are 16 clocks
+    // each) would hold up the next product, on all wavefronts at once.  (Left to itself the compiler gathers them.)
+    constexpr int kProducts = FA * FB * (DT == BSP_F32 ? 4 : 1);
+    auto multiply = [&](const Operands &o, auto between) {
         if constexpr (DT == BSP_F32) {
             static_for<0, 4>([&](auto kk) {
                 constexpr int k = 2 * decltype(kk)::value;
@@ -154,35 +159,51 @@ __global__ __launch_bounds__(64 * WA * WB) void fp8_tile_kernel(Product p) {
                 for (int i = 0; i < FA; ++i) wa8[i] = widen8((uint32_t)o.a[i][k], (uint32_t)o.a[i][k + 1], sc[i]);
 #pragma unroll
                 for (int j = 0; j < FB; ++j) wb8[j] = widen8((uint32_t)o.b[j][k], (uint32_t)o.b[j][k + 1], sc[FA + j]);
-#pragma unroll
-                for (int i = 0; i < FA; ++i)
-#pragma unroll
-                    for (int j = 0; j < FB; ++j) acc[i][j] = mfma32<BSP_BF16>(wa8[i], wb8[j], acc[i][j]);
+                static_for<0, FA * FB>([&](auto n) {
+                    constexpr int i = decltype(n)::value / FB, j = decltype(n)::value % FB;
+                    acc[i][j] = mfma32<BSP_BF16>(wa8[i], wb8[j], acc[i][j]);
+                    between(std::integral_constant<int, decltype(kk)::value * FA * FB + decltype(n)::value>{});
+                });
             });
         } else {
-#pragma unroll
-            for (int i = 0; i < FA; ++i)
-#pragma unroll
-                for (int j = 0; j < FB; ++j) acc[i][j] = mfma_scaled(o.a[i], o.b[j], acc[i][j], sc[i], sc[FA + j]);
+            static_for<0, FA * FB>([&](auto n) {
+                constexpr int i = decltype(n)::value / FB, j = decltype(n)::value % FB;
+                acc[i][j] = mfma_scaled(o.a[i], o.b[j], acc[i][j], sc[i], sc[FA + j]);
+                between(n);
+            });
         }
+        __builtin_amdgcn_sched_barrier(0);
     };
-    constexpr int kEach = kLoads + kScaleLoads;
+    auto nothing = [](auto) {};
+    // n others dealt evenly over the products
+    auto dealt = [&](auto n, auto other) {
+        return [=](auto product) {
+            constexpr int N = decltype(n)::value, P = decltype(product)::value;
+            static_for<P * N / kProducts, (P + 1) * N / kProducts>([&](auto o) { other(o); });
+            __builtin_amdgcn_sched_barrier(0);
+        };
+    };
+    using Others = std::integral_constant<int, kEach>;
     int slot = 0;
     if constexpr (NS == 2) {
-        for (int s = first; s < last; ++s) {
+        auto step = [&](int s, auto more) {
             wait_loads<0>();
             barrier();  // this step is in LDS, and nobody reads the other slot any more
-            if (s + 1 < last) load(s + 1, slot ^ 1);
             read_scales(slot);
-#pragma unroll
-            for (int sub = 0; sub < 2; ++sub) {
-                Operands o;
-                read(o, slot, sub);
-                multiply(o);
-            }
+            constexpr bool kBoth = DT != BSP_F32 || FA * FB < 8;  // both halves are read at once, where the registers have room for them
+            Operands o[kBoth ? 2 : 1];
+            read(o[0], slot, 0);
+            if constexpr (kBoth) read(o[1], slot, 1);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (decltype(more)::value) multiply(o[0], dealt(Others{}, [&](auto i) { load_one(i, s + 1, slot ^ 1); }));
+            else multiply(o[0], nothing);
+            if constexpr (!kBoth) read(o[0], slot, 1);
+            multiply(o[kBoth ? 1 : 0], nothing);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             slot ^= 1;
-        }
+        };
+        for (int s = first; s + 1 < last; ++s) step(s, std::true_type{});
+        step(last - 1, std::false_type{});
     } else {
         // The first half of a step is read while the second half of the one before it is multiplied: a step is in LDS, for everybody, half a
         // step before its turn.
@@ -195,19 +216,18 @@ __global__ __launch_bounds__(64 * WA * WB) void fp8_tile_kernel(Product p) {
         // (The products stay on their side of the barrier: the compiler would move them behind it, where everything waits for everything.)
         auto step = [&](int s, auto behind) {  // behind: whether all the steps that the ring has room for are behind this one
             constexpr bool kFull = decltype(behind)::value;
-            const int next = slot == NS - 1 ? 0 : slot + 1;
-            if (kFull) load(s + NS - 1, slot == 0 ? NS - 1 : slot - 1);
+            const int next = slot == NS - 1 ? 0 : slot + 1, free = slot == 0 ? NS - 1 : slot - 1;
             read(o[1], slot, 1);
             __builtin_amdgcn_sched_barrier(0);
-            multiply(o[0]);
-            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (kFull) multiply(o[0], dealt(Others{}, [&](auto i) { load_one(i, s + NS - 1, free); }));
+            else multiply(o[0], nothing);
             // the next step's loads are done where no more are left than those of the steps behind it
             wait_loads<kFull ? (NS - 2) * kEach : 0>();
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             barrier();
             if (kFull || s + 1 < last) read(o[0], next, 0);
             __builtin_amdgcn_sched_barrier(0);
-            multiply(o[1]);
+            multiply(o[1], nothing);
             if (kFull || s + 1 < last) read_scales(next);
             slot = next;
         };
