@@ -213,14 +213,17 @@ __device__ __forceinline__ float nearest_root(float v) {
     return __builtin_fmaf(-up, s, v) > 0.0f ? up : r;
 }
 
-// |y| <= 448 to one of the two codes' values next to it, up where the 16 bits (of 2^16) exceed what is missing.  Below 2^-6 the
-// step is that of 2^-6, which the addition of 2^-6 brings about.
-__device__ __forceinline__ float round_random(float y, uint32_t bits16) {
-    const float a = __builtin_fabsf(y);
-    const bool small = a < 0.015625f;
-    const float z = small ? a + 0.015625f : a;
-    const float q = __uint_as_float((__float_as_uint(z) + (bits16 << 4)) & 0xfff00000u);
-    return __builtin_copysignf(small ? q - 0.015625f : q, y);
+// |y| <= 448 to one of the two codes' values next to it, up where what y has above the lower one and the 16 bits (of 2^16) make a whole step.
+// From 2^-6 on the carry out of the 20 bits that the code does not have says so.  Below it a step is 2^-9, and a comparison decides (an addition
+// would round, and one code in a million would differ from what it has to be); few values are so far below their block's largest, so that is
+// looked for in a wavefront as a whole.
+constexpr float kLeastNormal = 0.015625f;
+__device__ __forceinline__ float round_normal(float a, uint32_t bits16) {
+    return __uint_as_float((__float_as_uint(a) + (bits16 << 4)) & 0xfff00000u);
+}
+__device__ __forceinline__ float round_small(float a, uint32_t bits16) {
+    const float t = a * 512.0f, whole = __builtin_floorf(t), missing = (float)(65536u - bits16) * 0x1p-16f;
+    return (t - whole >= missing ? whole + 1.0f : whole) * 0x1p-9f;
 }
 
 // four values, each an e4m3 number, as codes
@@ -331,13 +334,29 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(Table tab, Hyper h) {
         // (2^-100: below it 448 / largest has no number, and such moments move nothing)
         const bool has_m = top_m >= 0x1p-100f, has_r = top_r >= 0x1p-100f;
         const float im = has_m ? 448.0f * (1.0f / top_m) : 0.0f, ir = has_r ? 448.0f * (1.0f / top_r) : 0.0f;
+        uint32_t bits[4];
+        float ym[4], yr[4];  // (y of m with its sign)
+        bool small = false;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t bits = mix((uint32_t)(i0 + j) + s.salt);
-            const float ym = __builtin_fminf(__builtin_fmaxf(m[j] * im, -448.0f), 448.0f), yr = __builtin_fminf(r[j] * ir, 448.0f);
-            m[j] = round_random(ym, bits & 0xffffu);
-            r[j] = yr > 0.0f ? __builtin_fmaxf(round_random(yr, bits >> 16), 0x1p-9f) : 0.0f;
+            bits[j] = mix((uint32_t)(i0 + j) + s.salt);
+            ym[j] = __builtin_fminf(__builtin_fmaxf(m[j] * im, -448.0f), 448.0f);
+            yr[j] = __builtin_fminf(r[j] * ir, 448.0f);
+            m[j] = round_normal(__builtin_fabsf(ym[j]), bits[j] & 0xffffu);
+            r[j] = round_normal(yr[j], bits[j] >> 16);
+            small |= __builtin_fminf(__builtin_fabsf(ym[j]), yr[j]) < kLeastNormal;
         }
+        if (__ballot(small)) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float a = __builtin_fabsf(ym[j]);
+                m[j] = a < kLeastNormal ? round_small(a, bits[j] & 0xffffu) : m[j];
+                const float least = yr[j] > 0.0f ? __builtin_fmaxf(round_small(yr[j], bits[j] >> 16), 0x1p-9f) : 0.0f;
+                r[j] = yr[j] < kLeastNormal ? least : r[j];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) m[j] = __builtin_copysignf(m[j], ym[j]);
         const uint32_t mn = codes4(m), vn = codes4(r);
         if (lane == 0) {
             e.scales[block] = has_m ? top_m * (1.0f / 448.0f) : 0.0f;
