@@ -11,6 +11,9 @@
 // thousandth in a step, a code by a sixteenth, and rounded to the nearest a moment would never move.  The random bits are mixed from the
 // element's place, the step and the seed, so equal calls give equal bits.  A positive r does not become 0: the next step
 // would divide by eps alone.
+//
+// Both are bound by memory.  Measured (MI355X, us): 302 M weights of 288 tensors with masks, 16-bit gradients and copies, fp32 moments 1830 (4.6 TB/s of
+// 28 bytes a weight), 8-bit ones 1031 (4.7 of 16; some 90 vector instructions a weight, about what the memory leaves time for); 750000 weights 6.5.
 #include "bsp_common.h"
 
 #include <algorithm>

@@ -6,8 +6,10 @@
 // scales there, and a code times its scale has no rounding of its own.  Against a scale of largest / 448 it leaves at most one of the
 // type's 18 binades unused.
 //
-// Bound by memory.  Row segments alone: 16 lanes to a segment.  Else a workgroup reads a 128 x 128 tile once, 8 x 8 values per thread, and has from it the row segments, the column
-// segments (the rows of the transposed matrix) or the block, and the codes of either orientation; the transposed ones go through LDS.
+// Bound by memory.  Row segments alone: 16 lanes to a segment.  Else a workgroup reads a 128 x 128 tile once, 4 x 8 values per thread, and has
+// from it the row segments, the column segments (the rows of the transposed matrix) or the block, and the codes of either
+// orientation; the transposed ones go through LDS.  Measured (MI355X, bf16, us): 16384 x 4096 by rows 33 (6.0 TB/s), 8192 x 1024 7.3; in both
+// orientations 8192 x 4096 by rows 30 to 34 (4.2 TB/s), in blocks 28.5; 64 x 1024 by rows 2.5.
 #include "bsp_common.h"
 #include "bsp_fp8_device.h"
 
