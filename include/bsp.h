@@ -187,8 +187,9 @@ int bsp_adam_step(float *W, const void *G, int gdt, float *m, float *v, int64_t 
  *   floats further on, the largest r, each divided by 448: a moment is its code times its block's scale.  A new moment goes to
  *   one of its two neighbouring codes at random, in proportion to its distance, with 16 bits each for m and r mixed from the
  *   element's index in its tensor, t and seed: equal calls give equal bits.  r > 0 is stored as the least positive code at
- *   least; a block whose largest value is below 2^-100 as zeros.  The update itself uses the moments before they are
- *   stored.  All-zero codes and scales are a fresh state.
+ *   least; a block whose largest value is below 2^-100 as zeros.  A block in which a moment is not finite (a gradient that was
+ *   not, or whose square has no fp32 number) gets scales of 0: its elements start afresh.  The update itself uses the moments
+ *   before they are stored.  All-zero codes and scales are a fresh state.
  * tensors: HOST array of `count` descriptions, read during the call; device pointers in it.  Tensors are [M, N] row-major and
  *   contiguous (a vector: M = 1), of any size, 0 included; keep and alpha are [M / R, N], R is read only with them.
  *   No two tensors of a call may overlap (weights that do, a tied tensor listed twice, are refused).  Addresses need

@@ -334,8 +334,10 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(Table tab, Hyper h) {
             bits_r = bits_r > ur ? bits_r : ur;
         }
         const float top_m = wave_max(bits_m), top_r = wave_max(bits_r);
-        // (2^-100: below it 448 / largest has no number, and such moments move nothing)
-        const bool has_m = top_m >= 0x1p-100f, has_r = top_r >= 0x1p-100f;
+        // (2^-100: below it 448 / largest has no number, and such moments move nothing.  A block with a moment that is not finite starts afresh: a
+        // scale of infinity would make all its other weights NaN in the next step, zeros of r alone would let m move them without bound.)
+        const bool finite = top_m <= 3.402823466e38f && top_r <= 3.402823466e38f;
+        const bool has_m = finite && top_m >= 0x1p-100f, has_r = finite && top_r >= 0x1p-100f;
         const float im = has_m ? 448.0f * (1.0f / top_m) : 0.0f, ir = has_r ? 448.0f * (1.0f / top_r) : 0.0f;
         uint32_t bits[4];
         float ym[4], yr[4];  // (y of m with its sign)

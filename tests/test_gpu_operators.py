@@ -515,6 +515,27 @@ def test_adamw_flushes_what_has_no_scale_and_starts_fresh():
     assert not s[0][:, 0].any() and (s[0][:, 1] > 0).all() and not m[0].view(torch.uint8)[:256].any()
 
 
+def test_adamw_8bit_block_with_a_moment_that_is_not_finite_starts_afresh():
+    """One gradient of infinity, NaN or more than the root of fp32's range leaves the other weights of its block finite, then and later; a
+    step from fresh moments at t = 3 is lr (0.1 / 0.271) / sqrt(0.001 / 0.002997) = 0.639 lr."""
+    n, lr = 1024, 1e-2
+    w = [torch.ones(n, device="cuda")]
+    m, v, s = bsp.bsp_adamw_state(w, 8)
+    g = torch.linspace(0.5, 1.5, n, device="cuda")
+    bsp.bsp_adamw_step(w, [g], m, v, lr, t=1, scales=s, **HYPER)
+    bad = g.clone()
+    bad[10], bad[300], bad[700] = 1e30, float("inf"), float("nan")
+    bsp.bsp_adamw_step(w, [bad], m, v, lr, t=2, scales=s, **HYPER)
+    lost = torch.zeros(n, dtype=torch.bool, device="cuda")
+    lost[300] = lost[700] = True
+    assert torch.equal(w[0].isnan(), lost) and w[0].isfinite().sum() == n - 2
+    assert (s[0][:, :3] == 0).all() and (s[0][:, 3] > 0).all()
+    before = w[0].clone()
+    bsp.bsp_adamw_step(w, [g], m, v, lr, t=3, scales=s, **HYPER)
+    moved = (w[0] - before)[~lost].abs()
+    assert torch.equal(w[0].isnan(), lost) and float((moved[:766] / (0.639 * lr) - 1).abs().max()) < 1e-2 and (s[0] > 0).all()
+
+
 def test_adamw_refuses_what_does_not_fit():
     w = torch.zeros(32, 16, device="cuda")
     ok = lambda **k: bsp.bsp_adamw_step(**{**dict(W=[w], G=[w.clone()], m=[w.clone()], v=[w.clone()], lr=1e-3), **k})  # noqa: E731
