@@ -195,7 +195,7 @@ int bsp_adam_step(float *W, const void *G, int gdt, float *m, float *v, int64_t 
  *   No two tensors of a call may overlap (weights that do, a tied tensor listed twice, are refused).  Addresses need
  *   their element's alignment.
  * lr_t: NULL, or two device floats {lr, t} that the kernels read in the place of the arguments: a step that was captured in
- *   a graph is replayed with new ones (t as a float: exact up to 2^24).  A captured step without it repeats its t, and its random bits.
+ *   a graph is replayed with new ones (t as a float, 1 or more: exact up to 2^24).  A captured step without it repeats its t, and its random bits.
  * Up to 40 tensors are one launch.  Errors: BSP_ERR_NULL, BSP_ERR_DTYPE (gdt; cdt other than bf16 / fp16),
  * BSP_ERR_SHAPE (state_bits, t < 1 without lr_t, negative sizes, N >= 2^31, 2^34 elements or more, M % R != 0 with
  * keep or alpha, misalignment,
@@ -426,7 +426,7 @@ int bsp_linear_planned_fused(const void *X, int xdt, int64_t T, int64_t M, int64
  *   BSP_NORM_POST and dgate only, dH, Z and stats_pre for BSP_NORM_PRE only.  dX and dF may be dZ or dH (not each other).
  * ws: bsp_block_norm_backward_workspace_bytes(T, H, gate_rows) bytes (gate_rows 0 without a gate), 256-byte aligned,
  *   undefined before and after; calls that may overlap need one each.  Only needed where a sum down the rows is asked for.
- * T == 0: nothing, and sums of zero.  Errors: BSP_ERR_NULL, BSP_ERR_DTYPE (dt, kind, norms), BSP_ERR_SHAPE (H outside 1 ..
+ * T == 0: nothing, and sums of zero (of up to 65531 gate rows).  Errors: BSP_ERR_NULL, BSP_ERR_DTYPE (dt, kind, norms), BSP_ERR_SHAPE (H outside 1 ..
  * 8192, T >= 2^31, gate_rows, a gradient of what is absent, misalignment), BSP_ERR_CAPACITY (ws_bytes). */
 typedef enum { BSP_NORM_LAYER = 0, BSP_NORM_RMS = 1 } bsp_norm_kind;
 typedef enum { BSP_NORM_POST = 1, BSP_NORM_PRE = 2 } bsp_norm_place;
@@ -468,8 +468,9 @@ int bsp_block_norm_backward(const void *dZ, const void *dH, const void *Z, const
  * the same bits; bias, residual and Y have type xdt.  ws: bsp_linear_fp8_workspace_bytes(T, M, N) bytes (0 where few
  * tokens are quantised on the way), 256-byte aligned.
  *
- * rows, T may be 0 (nothing is done); K <= 2^23.  Errors: BSP_ERR_NULL, BSP_ERR_DTYPE (types, layout, act), BSP_ERR_SHAPE (sizes,
- * A, B, Q, Qt not 16-byte aligned, others not by their element), BSP_ERR_CAPACITY (ws_bytes too small). */
+ * residual may be Y; other overlaps of results and operands are not allowed.  rows, T may be 0 (nothing is done); K <= 2^23;
+ * launches are of less than 2^32 threads: 2^36 padded elements to quantise, 2^27 rows of B, 2^30 of A are refused.  Errors: BSP_ERR_NULL,
+ * BSP_ERR_DTYPE (types, layout, act), BSP_ERR_SHAPE (sizes, A, B, Q, Qt not 16-byte aligned, others not by their element), BSP_ERR_CAPACITY (ws_bytes too small). */
 typedef enum { BSP_FP8_ROW = 0, BSP_FP8_BLOCK = 1 } bsp_fp8_layout;
 int bsp_fp8_quant(const void *X, int xdt, int64_t rows, int64_t cols, int layout, void *Q, uint8_t *S, void *Qt, uint8_t *St,
                   void *stream);

@@ -541,7 +541,7 @@ int check(int64_t T, int64_t H, int dt, int norms, int kind, const void *gate, i
     if (norms < 1 || norms > 3) return BSP_ERR_DTYPE;
     if (T < 0 || H <= 0 || H > kMaxH || T >= ((int64_t)1 << 31)) return BSP_ERR_SHAPE;
     if (gate && (gate_rows < 1 || T % gate_rows != 0 || gate_rows > 0x7fffffff)) return BSP_ERR_SHAPE;
-    if (gate && T && gate_rows > T) return BSP_ERR_SHAPE;
+    if (gate && gate_rows > (T ? T : 65535 - kDgate)) return BSP_ERR_SHAPE;  // (of no rows: the launch that clears the sums has a line of workgroups for each)
     return BSP_OK;
 }
 

@@ -470,7 +470,7 @@ struct Shape {
     int splits, split_steps;
 };
 
-// Microseconds of a product in `n` tiles (with the splits) of `steps` steps; fitted to 60 shapes of 32 to 16384 rows and 1024 to 16384
+// Microseconds of a product in `n` tiles (with the splits) of `steps` steps; fitted to sweeps over 32 to 16384 rows and 1024 to 16384
 // columns.  `wide`: fp32 results, whose instructions take twice as long.  A larger tile loads less for a product, but its
 // workgroups leave compute units idle at the end of a round, and one of 256 x 256 fills a compute unit, so that its epilogue (GELU: 8 us a round)
 // hides nothing.  Two steps in LDS let two workgroups of 128 x 128 share a compute unit and wait for each other; with three
@@ -524,7 +524,7 @@ int launch_tile(const Product &p, int splits, hipStream_t s) {
         }
     }
     const int64_t wgs = ((p.T + TB - 1) / TB + 7) / 8 * 8 * ((p.M + TA - 1) / TA);
-    if (wgs >= ((int64_t)1 << 31)) return BSP_ERR_SHAPE;
+    if (wgs * splits * (64 * WA * WB) >= ((int64_t)1 << 32)) return BSP_ERR_SHAPE;
     k<<<dim3((unsigned)wgs, (unsigned)splits), 64 * WA * WB, lds, s>>>(p);
     return check_launch();
 }
@@ -532,6 +532,7 @@ int launch_tile(const Product &p, int splits, hipStream_t s) {
 template <int DT, bool RAW>
 int launch_few(const Product &p, const void *X, int64_t N, hipStream_t s) {
     const unsigned grid = (unsigned)((p.M + 15) / 16), threads = 64u * (unsigned)(p.steps < kFewWaves ? p.steps : kFewWaves);
+    if ((uint64_t)grid * threads >= ((uint64_t)1 << 32)) return BSP_ERR_SHAPE;
     if (p.T <= 16) fp8_few_kernel<DT, 1, RAW><<<grid, threads, 0, s>>>(p, X, N);
     else fp8_few_kernel<DT, 2, RAW><<<grid, threads, 0, s>>>(p, X, N);
     return check_launch();

@@ -74,6 +74,18 @@ def test_block_norm_refusals():
     assert q(0, 64, 0) == 0 and q(4, 9000, 0) == 0 and q(4, 64, 3) == 0 and q(4, 64, 4) > 0 and q(100000, 1024, 0) > q(10, 1024, 0)
 
 
+def test_what_no_launch_can_hold_is_refused():
+    """2^32 threads or more, or more lines of workgroups than a grid has."""
+    L = bsp.lib()
+    assert L.bsp_fp8_quant(P, 1, 1 << 30, 1, 0, P, P, None, None, None) == SHAPE
+    assert L.bsp_fp8_quant(P, 1, (1 << 31) - 1, 4096, 0, P, P, None, None, None) == SHAPE
+    mm = lambda T, M, K: L.bsp_matmul_fp8(P, P, P, P, 0, T, M, K, None, 0, None, P, 1, None, 0, None)  # noqa: E731
+    assert mm((1 << 31) - 1, 1, 128) == SHAPE and mm(1, 1 << 28, 1024) == SHAPE
+    assert L.bsp_linear_fp8(P, 1, 1, 1 << 28, 1024, P, P, 0, None, 0, None, P, P, 0, None) == SHAPE
+    assert L.bsp_block_norm_backward(P, P, P, P, 1, 0, 64, 3, 0, 1.0, P, 1 << 16, None, None, None, P, P, P, P, None, None, None, None, P, P, 1 << 20,
+                                     None) == SHAPE
+
+
 class _Tensor(C.Structure):
     _fields_ = [("w", C.c_void_p), ("g", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("scales", C.c_void_p), ("copy", C.c_void_p),
                 ("keep", C.c_void_p), ("alpha", C.c_void_p), ("M", C.c_int64), ("N", C.c_int64), ("R", C.c_int32), ("weight_decay", C.c_float)]
