@@ -56,7 +56,8 @@ __device__ __forceinline__ uint4 widen8(uint32_t lo, uint32_t hi, uint32_t scale
                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, f, true)));
 }
 
-// The tile's place: workgroup ids go round the 8 XCDs; each XCD owns whole groups of kGroup token tiles and walks their output ranges.
+// The tile's place: workgroup ids go round the 8 XCDs; each XCD has an eighth of the tiles in the order of groups of kGroup token tiles that walk
+// their output ranges.  (With whole token tiles for each XCD 88 tokens, two tiles, kept two of the eight busy.)
 constexpr uint32_t kGroup = 4;
 
 template <int DT, int FA, int FB, int WA, int WB, int NS>
@@ -72,12 +73,11 @@ __global__ __launch_bounds__(64 * WA * WB) void fp8_tile_kernel(Product p) {
     const int wa = wave % WA, wb = wave / WA;
 
     const uint32_t ranges = (uint32_t)((p.M + TA - 1) / TA), tiles = (uint32_t)((p.T + TB - 1) / TB);
-    const uint32_t per_xcd = (tiles + 7) / 8, place = blockIdx.x >> 3;
+    const uint32_t n = tiles * ranges, place = (blockIdx.x & 7) * ((n + 7) / 8) + (blockIdx.x >> 3);
+    if (place >= n || (blockIdx.x >> 3) >= (n + 7) / 8) return;  // uniform: before any barrier
     const uint32_t group = place / (kGroup * ranges), in_group = place - group * kGroup * ranges;
-    const uint32_t height = per_xcd - group * kGroup < kGroup ? per_xcd - group * kGroup : kGroup;
-    const uint32_t tile = (group * kGroup + in_group % height) * 8 + (blockIdx.x & 7);
-    const int64_t t0 = (int64_t)tile * TB, m0 = (int64_t)(in_group / height) * TA;
-    if (t0 >= p.T) return;  // uniform: before any barrier
+    const uint32_t height = tiles - group * kGroup < kGroup ? tiles - group * kGroup : kGroup;
+    const int64_t t0 = (int64_t)(group * kGroup + in_group % height) * TB, m0 = (int64_t)(in_group / height) * TA;
     const int first = blockIdx.y * p.split_steps, last = first + p.split_steps < p.steps ? first + p.split_steps : p.steps;
 
     // the loads of this wavefront: 8 rows each, first B's, then A's; a row past the end reads the last one
@@ -539,7 +539,7 @@ int launch_tile(const Product &p, int splits, hipStream_t s) {
             return BSP_ERR_HIP;
         }
     }
-    const int64_t wgs = ((p.T + TB - 1) / TB + 7) / 8 * 8 * ((p.M + TA - 1) / TA);
+    const int64_t wgs = ((p.T + TB - 1) / TB * ((p.M + TA - 1) / TA) + 7) / 8 * 8;
     if (wgs * splits * (64 * WA * WB) >= ((int64_t)1 << 32)) return BSP_ERR_SHAPE;
     k<<<dim3((unsigned)wgs, (unsigned)splits), 64 * WA * WB, lds, s>>>(p);
     return check_launch();
