@@ -486,23 +486,31 @@ struct Shape {
     int splits, split_steps;
 };
 
-// Microseconds of a product in `n` tiles (with the splits) of `steps` steps; fitted to sweeps over 32 to 16384 rows and 1024 to 16384
-// columns.  `wide`: fp32 results, whose instructions take twice as long.  A larger tile loads less for a product, but its
-// workgroups leave compute units idle at the end of a round, and one of 256 x 256 fills a compute unit, so that its epilogue (GELU: 8 us a round)
-// hides nothing.  Two steps in LDS let two workgroups of 128 x 128 share a compute unit and wait for each other; with three
-// a workgroup that is alone on it reads half a step ahead.  Measured, 256 / 128 / 127 / 64 / 63: 16384 x 4096, K = 4096 234 / 268 / - / 418 / -; 8192 x
-// 4096, K = 1024 45 / 47 / 62 / 63 / 79, with GELU 58 / 53 / - / 68; 2048 x 1024, K = 4096 50 / 27 / 19 / 20 / 18; 512 x 1024, K = 4096 50 / 26 / 19 / 20 /
-// 11.9; 1024 x 4096, K = 8192 in fp32 166 / 82 / 72 / 88 / 92.
+// Rounds of `n` workgroups of which the compute units take `together` at once; in the last one up to 256 have a compute unit each and take
+// `alone` of a round.
+double rounds_of(double n, double together, double alone) {
+    const double whole = __builtin_floor(n / together), left = n - whole * together;
+    return left == 0.0 ? whole : whole + alone + (1.0 - alone) * (left > 256.0 ? (left - 256.0) / (together - 256.0) : 0.0);
+}
+
+// Microseconds of a product in `n` tiles (with the splits) of `steps` steps; fitted to 127 shapes of 33 to 16384 rows, 64 to 8192 outputs and 64 to
+// 16384 columns, where the tile that is chosen takes 1 % longer than the best one in the mean (3 % at
+// 115 others).  `wide`: fp32 results, whose instructions take
+// twice as long.  A larger tile loads less for a product, but its workgroups leave compute units idle at the end of a round, and one of 256 x 256
+// fills a compute unit, so that its epilogue (GELU: 8 us a round) hides nothing.  Two steps in LDS let two workgroups of 128 x 128 share a compute
+// unit and wait for each other; with three a workgroup that is alone on it reads half a step ahead.  Measured, 256 / 128 / 127 / 64 / 63: 16384 x
+// 4096, K = 4096 231 / 280 / 315 / 438 / 442; 8192 x 4096, K = 1024 44 / 44 / 62 / 66 / 82, with GELU 58 / 55 / 73 / 75 / 94; 2048 x 1024, K = 4096
+// 49 / 28 / 20 / 22 / 18; 512 x 1024, K = 4096 49 / 28 / 19 / 21 / 11; 1024 x 4096, K = 8192 in fp32 150 / 79 / 68 / 90 / 87.
 double tile_us(int tile, double n, double steps, bool wide, bool gelu) {
-    const double rounds = __builtin_ceil(n / 256.0), pairs = __builtin_ceil(n / 512.0);
+    const double rounds = __builtin_ceil(n / 256.0);
     switch (tile) {
-        case 256: return 5.0 + rounds * ((wide ? 3.2 : 1.62) * steps + 5.0 + (gelu ? 8.5 : 0.0));
-        case 128: return 3.5 + pairs * ((wide ? 1.85 : 1.03) * steps + 2.2 + (gelu ? 2.5 : 0.0));
-        case 127: return 3.5 + rounds * ((wide ? 1.04 : n <= 256.0 ? 0.46 : 0.62) * steps + 1.5 + (gelu ? 2.5 : 0.0));
-        case 64: return 3.5 + __builtin_ceil(n / 1024.0) * ((wide ? 1.25 : 0.83) * steps + 1.6 + (gelu ? 1.0 : 0.0));
+        case 256: return 4.0 + rounds * ((wide ? 2.95 : 1.46) * steps + 5.0 + (gelu ? 10.0 : 0.0));
+        case 128: return 4.0 + rounds_of(n, 512.0, 0.6) * ((wide ? 2.1 : 0.98) * steps + 3.0 + (gelu ? 2.0 : 0.0));
+        case 127: return 4.0 + rounds * ((wide ? 0.98 : n <= 256.0 ? 0.37 : 0.54) * steps + 2.7 + (gelu ? 1.0 : 0.0));
+        case 64: return 4.0 + rounds_of(n, 1024.0, 0.42) * ((wide ? 1.28 : 0.8) * steps + 1.6 + (gelu ? 1.5 : 0.0));
         default:
-            if (n <= 256.0) return 5.0 + (wide ? 0.41 : 0.215) * steps;
-            return 3.5 + pairs * ((wide ? 0.75 : 0.41) * steps + 1.8 + (gelu ? 0.5 : 0.0));
+            if (n <= 256.0) return 5.0 + (wide ? 0.49 : 0.215) * steps;
+            return 4.0 + rounds_of(n, 512.0, 0.61) * ((wide ? 0.68 : 0.36) * steps + 2.2 + (gelu ? 0.5 : 0.0));
     }
 }
 
@@ -518,7 +526,7 @@ Shape choose(int64_t T, int64_t M, int64_t steps, bool wide, bool gelu) {
             if (k > 1 && (steps < 4 * k || n * k > 512.0)) break;
             const int64_t each = (steps + k - 1) / k;
             double us = tile_us(tile, n * k, (double)each, wide, gelu);
-            if (k > 1) us += 4.5 + (double)T * (double)M * (8.0 * k + 4.0) / 5e6;
+            if (k > 1) us += 4.7 + (double)T * (double)M * (8.0 * k + 4.0) / 4.3e6;
             if (least != 0.0 && us >= least) continue;
             least = us;
             best = {tile, (int)((steps + each - 1) / each), (int)each};
