@@ -41,8 +41,7 @@ struct Entry {
     const float *alpha;
     int64_t n;
     uint32_t N, R;
-    float decay;       // lr * weight decay where the host knows lr, else the weight decay
-    uint32_t aligned;  // four elements at a time
+    float decay;  // lr * weight decay where the host knows lr, else the weight decay
 };
 
 struct Table {
@@ -250,7 +249,6 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(Table tab, Hyper h) {
     const bool grouped = e.keep || e.alpha;
     Groups groups(e, grouped ? base : 0);
     if (grouped) groups.advance(4 * lane);
-    const bool one_row = (e.N & 3) == 0;  // a lane's four elements are neighbours in the group arrays
     const int64_t blocks = (e.n + kBlock - 1) / kBlock;
     const float decay = h.lr_t ? s.lr * e.decay : e.decay, rate = s.lr / s.c1, root = 1.0f / __builtin_sqrtf(s.c2);
     uint8_t *m8 = (uint8_t *)e.m, *v8 = (uint8_t *)e.v;
@@ -258,20 +256,18 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(Table tab, Hyper h) {
         const int64_t i0 = base + b * kBlock + 4 * lane, block = base / kBlock + b;
         if (block >= blocks) break;  // uniform in a wavefront
         const int have = e.n - i0 >= 4 ? 4 : (e.n > i0 ? (int)(e.n - i0) : 0);
-        const bool four = e.aligned && have == 4;
+        const bool four = have == 4;  // (loads and stores of several elements need no alignment here)
         float w[4] = {0, 0, 0, 0}, g[4] = {0, 0, 0, 0}, m[4], r[4];
         uint32_t mc = 0, vc = 0;
         if (four) {
-            const float4 t = *reinterpret_cast<const float4 *>(e.w + i0);
-            w[0] = t.x, w[1] = t.y, w[2] = t.z, w[3] = t.w;
-            mc = *reinterpret_cast<const uint32_t *>(m8 + i0);
-            vc = *reinterpret_cast<const uint32_t *>(v8 + i0);
+            __builtin_memcpy(w, e.w + i0, 16);
+            __builtin_memcpy(&mc, m8 + i0, 4);
+            __builtin_memcpy(&vc, v8 + i0, 4);
             if constexpr (GDT == BSP_F32) {
-                const float4 u = *reinterpret_cast<const float4 *>((const float *)e.g + i0);
-                g[0] = u.x, g[1] = u.y, g[2] = u.z, g[3] = u.w;
+                __builtin_memcpy(g, (const float *)e.g + i0, 16);
             } else {
-                const uint2 u = *reinterpret_cast<const uint2 *>((const uint16_t *)e.g + i0);
-                const uint16_t c[4] = {(uint16_t)u.x, (uint16_t)(u.x >> 16), (uint16_t)u.y, (uint16_t)(u.y >> 16)};
+                uint16_t c[4];
+                __builtin_memcpy(c, (const uint16_t *)e.g + i0, 8);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) g[j] = elem<GDT>::load(&c[j], 0);
             }
@@ -293,22 +289,31 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(Table tab, Hyper h) {
         if (grouped) {
             Groups at = groups;
             groups.advance(kBlock);
-            if (four && one_row) {
+            if (four && at.col + 4 <= at.N) {  // neighbours in the group arrays
                 if (e.keep) {
                     uint32_t k4;
                     __builtin_memcpy(&k4, e.keep + at.at(), 4);
                     kept = ((k4 & 0xffu) != 0) | ((k4 & 0xff00u) != 0) << 1 | ((k4 & 0xff0000u) != 0) << 2 | ((k4 & 0xff000000u) != 0) << 3;
                 }
                 if (e.alpha) __builtin_memcpy(coef, e.alpha + at.at(), 16);
-            } else {
-                kept = 0u;
-                for (int j = 0; j < have; ++j) {
-                    if (!e.keep || e.keep[at.at()]) kept |= 1u << j;
-                    const float c = e.alpha ? e.alpha[at.at()] : 0.0f;
+            } else if (have) {  // (a row ends among them, or the tensor: all places, then all loads)
+                int64_t place[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) coef[k] = k == j ? c : coef[k];
+                for (int j = 0; j < 4; ++j) {
+                    place[j] = j < have ? at.at() : place[0];
                     at.advance(1);
                 }
+                if (e.keep) {
+                    uint8_t k[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) k[j] = e.keep[place[j]];
+                    kept = 0u;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) kept |= (k[j] ? 1u : 0u) << j;
+                }
+                if (e.alpha)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) coef[j] = e.alpha[place[j]];
             }
         }
         uint32_t bits_m = 0, bits_r = 0;
@@ -368,12 +373,13 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(Table tab, Hyper h) {
             e.scales[blocks + block] = has_r ? top_r * (1.0f / 448.0f) : 0.0f;
         }
         if (four) {
-            *reinterpret_cast<float4 *>(e.w + i0) = make_float4(w[0], w[1], w[2], w[3]);
-            *reinterpret_cast<uint32_t *>(m8 + i0) = mn;
-            *reinterpret_cast<uint32_t *>(v8 + i0) = vn;
-            if (e.copy)
-                *reinterpret_cast<uint2 *>((uint16_t *)e.copy + i0) = make_uint2(elem<CDT>::bits(w[0]) | (elem<CDT>::bits(w[1]) << 16),
-                                                                                 elem<CDT>::bits(w[2]) | (elem<CDT>::bits(w[3]) << 16));
+            __builtin_memcpy(e.w + i0, w, 16);
+            __builtin_memcpy(m8 + i0, &mn, 4);
+            __builtin_memcpy(v8 + i0, &vn, 4);
+            if (e.copy) {
+                const uint2 c = make_uint2(elem<CDT>::bits(w[0]) | (elem<CDT>::bits(w[1]) << 16), elem<CDT>::bits(w[2]) | (elem<CDT>::bits(w[3]) << 16));
+                __builtin_memcpy((uint16_t *)e.copy + i0, &c, 8);
+            }
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -498,7 +504,6 @@ extern "C" int bsp_adamw_step(const bsp_adamw_tensor *tensors, int64_t count, in
         e.N = (uint32_t)x.N;
         e.R = (uint32_t)(x.R > 0 ? x.R : 1);
         e.decay = lr_t ? x.weight_decay : (float)(lr * (double)x.weight_decay);
-        e.aligned = aligned(x.w, 16) && aligned(x.g, 4 * dtype_size(gdt)) && aligned(x.m, 4) && aligned(x.v, 4) && aligned(x.copy, 8);
         tab.first[tab.count++] = (uint32_t)wgs;
         wgs += need;
     }
