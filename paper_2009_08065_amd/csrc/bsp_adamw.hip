@@ -27,9 +27,8 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxTensors = 40;            // 40 entries of 88 bytes: a launch has 4 KB of arguments
 constexpr int kBlock = 256;                // elements of an 8-bit scale: one wavefront, 4 per lane
-constexpr int kBlocksPerWave = 4;
 constexpr int64_t kMostWorkgroups = (int64_t)1 << 24;  // of a launch, which has less than 2^32 threads
-constexpr int64_t kChunk8 = (kThreads / kWave) * kBlocksPerWave * kBlock;
+constexpr int64_t kChunk8 = (kThreads / kWave) * kBlock;  // elements of a workgroup that has a block for each wavefront
 
 struct Entry {
     float *w;
@@ -238,21 +237,23 @@ __device__ __forceinline__ float value_of(uint32_t codes) {
     return __builtin_amdgcn_cvt_f32_fp8((int)codes, I);
 }
 
-template <int GDT, int CDT>
+// BLOCKS: blocks of a wavefront, one after the other: four for large models (302 M weights 1040 us, with one 1093), one where the launch would have
+// few workgroups (750000 weights of 12 tensors 7.8, with four 9.3; 10 layers of width 142 21, 29).
+template <int GDT, int CDT, int BLOCKS>
 __global__ __launch_bounds__(kThreads) void adamw8_kernel(Table tab, Hyper h) {
     Step s;
     if (!begin_step(h, s)) return;
     const int k = find_tensor(tab);
     const Entry &e = tab.e[k];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t base = (int64_t)(blockIdx.x - tab.first[k]) * kChunk8 + wave * (kBlocksPerWave * kBlock);
+    const int64_t base = (int64_t)(blockIdx.x - tab.first[k]) * (BLOCKS * kChunk8) + wave * (BLOCKS * kBlock);
     const bool grouped = e.keep || e.alpha;
     Groups groups(e, grouped ? base : 0);
     if (grouped) groups.advance(4 * lane);
     const int64_t blocks = (e.n + kBlock - 1) / kBlock;
     const float decay = h.lr_t ? s.lr * e.decay : e.decay, rate = s.lr / s.c1, root = 1.0f / __builtin_sqrtf(s.c2);
     uint8_t *m8 = (uint8_t *)e.m, *v8 = (uint8_t *)e.v;
-    for (int b = 0; b < kBlocksPerWave; ++b) {
+    for (int b = 0; b < BLOCKS; ++b) {
         const int64_t i0 = base + b * kBlock + 4 * lane, block = base / kBlock + b;
         if (block >= blocks) break;  // uniform in a wavefront
         const int have = e.n - i0 >= 4 ? 4 : (e.n > i0 ? (int)(e.n - i0) : 0);
@@ -395,7 +396,8 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(Table tab, Hyper h) {
 
 template <int GDT, int CDT>
 void launch(const Table &tab, const Hyper &h, unsigned wgs, int bits, int per, hipStream_t s) {
-    if (bits == 8) adamw8_kernel<GDT, CDT><<<wgs, kThreads, 0, s>>>(tab, h);
+    if (bits == 8 && per == 4) adamw8_kernel<GDT, CDT, 4><<<wgs, kThreads, 0, s>>>(tab, h);
+    else if (bits == 8) adamw8_kernel<GDT, CDT, 1><<<wgs, kThreads, 0, s>>>(tab, h);
     else if (per == 4) adamw32_kernel<GDT, CDT, 4><<<wgs, kThreads, 0, s>>>(tab, h);
     else adamw32_kernel<GDT, CDT, 2><<<wgs, kThreads, 0, s>>>(tab, h);
 }
@@ -436,7 +438,7 @@ extern "C" int bsp_adamw_step(const bsp_adamw_tensor *tensors, int64_t count, in
     if (count && !tensors) return BSP_ERR_NULL;
     if (!valid_dtype(gdt) || (cdt != BSP_BF16 && cdt != BSP_F16)) return BSP_ERR_DTYPE;
     if (!lr_t && t < 1) return BSP_ERR_SHAPE;
-    const int64_t largest = state_bits == 32 ? kThreads * 4 : kChunk8;
+    const int64_t largest = state_bits == 32 ? kThreads * 4 : 4 * kChunk8;
     int64_t all = 0;
     for (int64_t i = 0; i < count; ++i) {  // all of them before the first launch
         const bsp_adamw_tensor &x = tensors[i];
@@ -452,8 +454,8 @@ extern "C" int bsp_adamw_step(const bsp_adamw_tensor *tensors, int64_t count, in
             return BSP_ERR_SHAPE;
     }
     if (const int shared = overlapping(tensors, count)) return shared > 0 ? BSP_ERR_SHAPE : BSP_ERR_CAPACITY;
-    const int per = all >= 1024 * ((count + kMaxTensors - 1) / kMaxTensors) ? 4 : 2;
-    const int64_t chunk = state_bits == 32 ? kThreads * per : kChunk8;
+    const int per = all >= 1024 * ((count + kMaxTensors - 1) / kMaxTensors) ? 4 : (state_bits == 32 ? 2 : 1);
+    const int64_t chunk = per * (state_bits == 32 ? (int64_t)kThreads : kChunk8);
     Hyper h;
     h.lr = (float)lr;
     h.beta1 = (float)beta1;
