@@ -22,15 +22,20 @@ namespace {
 constexpr int kMaxH = 8192;
 constexpr int kVec = 8;  // values of a piece
 
-// Column of value j of piece u of thread t's share of a row.  WHOLE: a piece is 8 neighbouring columns, 16 or 32 bytes in one go (at any address: loads
-// and stores need no alignment).  Where the width is no multiple of 8 a piece is 8 columns a team's width apart (1536 x 770 in fp32, backward:
-// 22 us, 32 with whole pieces and one that ends inside).
-template <int TPR, bool WHOLE>
+// How a thread has its pieces of a row.  kWhole: 8 neighbouring columns, 16 or 32 bytes in one go (at any address: loads and stores need no
+// alignment).  kWords: the same from a buffer that ends with the row, word by word.  kApart: 8 columns a team's width apart.
+// Widths that are multiples of 8: kWords forward (us, 16384 x 4096 in fp32, both norms and gate rows 224, kWhole 239; 4096 x 2048 in bf16 15.8, 16.9),
+// kWhole backward (16384 x 4096 in fp32 378, kWords 403).  16-bit rows of an even width: kWords (353 x 6462 forward 10.3, kApart 12.9, backward 29.4,
+// 33.5; in fp32 it is the other way round, 12.3 and 11.3, 32.4 and 29.2).  Else kApart.
+enum { kApart, kWhole, kWords };
+
+// Column of value j of piece u of thread t's share of a row.
+template <int TPR, int HOW>
 __device__ __forceinline__ int column(int u, int j, int t) {
-    return WHOLE ? (u * TPR + t) * kVec + j : (u * kVec + j) * TPR + t;
+    return HOW != kApart ? (u * TPR + t) * kVec + j : (u * kVec + j) * TPR + t;
 }
 
-// The row of H elements at element `at`, as a buffer: past its end loads give 0 and stores write nothing.  (A team's row is the same for all
+// The row of H elements at element `at`, as a buffer: past its end loads give 0 and stores write nothing, word by word.  (A team's row is the same for all
 // lanes of a wavefront.  With a comparison and a branch for every element the kernel's code, which a short call runs through once, took
 // most of its time.)
 template <int SIZE>
@@ -41,26 +46,31 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of_row(const void *p, i
 }
 
 // A piece as it lies in memory.
-template <int DT, int TPR, bool WHOLE>
+template <int DT, int TPR, int HOW>
 struct Raw {
     uint4 d[DT == BSP_F32 ? 2 : 1];
     // of the row of H columns at element `at`
     __device__ __forceinline__ void load(const void *p, int64_t at, int u, int t, int H) {
         constexpr int size = DT == BSP_F32 ? 4 : 2;
-        if constexpr (WHOLE) {
-            const int c = column<TPR, true>(u, 0, t);
+        if constexpr (HOW == kWhole) {
+            const int c = column<TPR, HOW>(u, 0, t);
             if (c < H) {
                 __builtin_memcpy(d, (const uint8_t *)p + (at + c) * size, sizeof(d));
             } else {
 #pragma unroll
                 for (uint4 &x : d) x = make_uint4(0u, 0u, 0u, 0u);
             }
+        } else if constexpr (HOW == kWords) {
+            const __amdgpu_buffer_rsrc_t row = buffer_of_row<size>(p, at, H);
+            const int c = size * column<TPR, HOW>(u, 0, t);
+#pragma unroll
+            for (int i = 0; i < (int)(sizeof(d) / 16); ++i) d[i] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(row, c + 16 * i, 0, 0));
         } else {
             const __amdgpu_buffer_rsrc_t row = buffer_of_row<size>(p, at, H);
             uint32_t w[8];
 #pragma unroll
             for (int j = 0; j < kVec; ++j) {
-                const int c = size * column<TPR, false>(u, j, t);
+                const int c = size * column<TPR, HOW>(u, j, t);
                 if constexpr (DT == BSP_F32) w[j] = __builtin_amdgcn_raw_buffer_load_b32(row, c, 0, 0);
                 else w[j] = __builtin_amdgcn_raw_buffer_load_b16(row, c, 0, 0);
             }
@@ -84,10 +94,10 @@ struct Raw {
     }
 };
 
-template <int DT, int TPR, bool WHOLE>
+template <int DT, int TPR, int HOW>
 __device__ __forceinline__ void store_piece(const float (&v)[kVec], void *p, int64_t at, int u, int t, int H) {
-    if constexpr (WHOLE) {
-        const int c = column<TPR, true>(u, 0, t);
+    if constexpr (HOW == kWhole) {
+        const int c = column<TPR, HOW>(u, 0, t);
         if (c >= H) return;
         if constexpr (DT == BSP_F32) {
             __builtin_memcpy((float *)p + at + c, v, 32);
@@ -97,12 +107,24 @@ __device__ __forceinline__ void store_piece(const float (&v)[kVec], void *p, int
             for (int j = 0; j < 4; ++j) d[j] = cvt_pk<DT>(v[2 * j], v[2 * j + 1]);
             __builtin_memcpy((uint16_t *)p + at + c, d, 16);
         }
+    } else if constexpr (HOW == kWords) {
+        constexpr int size = DT == BSP_F32 ? 4 : 2;
+        const __amdgpu_buffer_rsrc_t row = buffer_of_row<size>(p, at, H);
+        const int c = size * column<TPR, HOW>(u, 0, t);
+        if constexpr (DT == BSP_F32) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])},
+                                                       row, c + 16 * i, 0, 0);
+        } else {
+            __builtin_amdgcn_raw_buffer_store_b128(u32x4{cvt_pk<DT>(v[0], v[1]), cvt_pk<DT>(v[2], v[3]), cvt_pk<DT>(v[4], v[5]), cvt_pk<DT>(v[6], v[7])}, row, c, 0, 0);
+        }
     } else {
         constexpr int size = DT == BSP_F32 ? 4 : 2;
         const __amdgpu_buffer_rsrc_t row = buffer_of_row<size>(p, at, H);
 #pragma unroll
         for (int j = 0; j < kVec; ++j) {
-            const int c = size * column<TPR, false>(u, j, t);
+            const int c = size * column<TPR, HOW>(u, j, t);
             if constexpr (DT == BSP_F32) __builtin_amdgcn_raw_buffer_store_b32(elem<DT>::bits(v[j]), row, c, 0, 0);
             else __builtin_amdgcn_raw_buffer_store_b16((uint16_t)elem<DT>::bits(v[j]), row, c, 0, 0);
         }
@@ -168,7 +190,7 @@ struct Forward {
 };
 
 // One team's row: mean and 1 / deviation of the values v (columns past the width hold 0 and are not part of it).
-template <int TPR, int ITER, bool WHOLE>
+template <int TPR, int ITER, int HOW>
 __device__ __forceinline__ void statistics(const float (&v)[ITER][kVec], int t, const Forward &a, float &mean, float &rstd, float *red, int &turn) {
     mean = 0.0f;
     const float n = 1.0f / (float)a.width;
@@ -187,13 +209,13 @@ __device__ __forceinline__ void statistics(const float (&v)[ITER][kVec], int t, 
 #pragma unroll
         for (int j = 0; j < kVec; ++j) {
             const float d = v[u][j] - mean;
-            q[0] = column<TPR, WHOLE>(u, j, t) < a.width ? __builtin_fmaf(d, d, q[0]) : q[0];
+            q[0] = column<TPR, HOW>(u, j, t) < a.width ? __builtin_fmaf(d, d, q[0]) : q[0];
         }
     team_sum<TPR, 1>(q, red, turn);
     rstd = 1.0f / __builtin_sqrtf(q[0] * n + a.eps);
 }
 
-template <int DT, int TPR, int ITER, bool WHOLE>
+template <int DT, int TPR, int ITER, int HOW>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void block_norm_kernel(Forward a) {
     constexpr int kTeams = TPR < 256 ? 256 / TPR : 1;
     __shared__ float red[TPR > 64 ? 2 * (TPR / 64) : 1];
@@ -204,7 +226,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void block_norm_kernel(Forwa
     const int64_t at = row * H;
     const bool post = a.F && (a.norms & BSP_NORM_POST), pre = (a.norms & BSP_NORM_PRE) != 0;
     // everything is asked for before the first sum is waited for
-    using Piece = Raw<DT, TPR, WHOLE>;
+    using Piece = Raw<DT, TPR, HOW>;
     Piece rx[ITER], rf[ITER], rg[ITER], w1[ITER], b1[ITER], w2[ITER], b2[ITER];
     auto ask = [&](Piece(&r)[ITER], const void *p, int64_t from) {
         if (p)
@@ -236,7 +258,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void block_norm_kernel(Forwa
             for (int j = 0; j < kVec; ++j) f[u][j] = rf[u][j];
         if (post) {
             float mean, rstd;
-            statistics<TPR, ITER, WHOLE>(f, t, a, mean, rstd, red, turn);
+            statistics<TPR, ITER, HOW>(f, t, a, mean, rstd, red, turn);
             if (a.stats_post && t == 0) *reinterpret_cast<float2 *>(a.stats_post + 2 * row) = make_float2(mean, rstd);
             normalise(f, mean, rstd, a.w_post, w1, a.b_post, b1);
         }
@@ -247,18 +269,18 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void block_norm_kernel(Forwa
         for (int j = 0; j < kVec; ++j) {
             float z = a.x_scale * rx[u][j];
             if (a.F) z += a.gate ? f[u][j] * rg[u][j] : f[u][j];
-            x[u][j] = column<TPR, WHOLE>(u, j, t) < H ? rounded<DT>(z) : 0.0f;
+            x[u][j] = column<TPR, HOW>(u, j, t) < H ? rounded<DT>(z) : 0.0f;
         }
     if (a.Z)
 #pragma unroll
-        for (int u = 0; u < ITER; ++u) store_piece<DT, TPR, WHOLE>(x[u], a.Z, at, u, t, H);
+        for (int u = 0; u < ITER; ++u) store_piece<DT, TPR, HOW>(x[u], a.Z, at, u, t, H);
     if (pre) {
         float mean, rstd;
-        statistics<TPR, ITER, WHOLE>(x, t, a, mean, rstd, red, turn);
+        statistics<TPR, ITER, HOW>(x, t, a, mean, rstd, red, turn);
         if (a.stats_pre && t == 0) *reinterpret_cast<float2 *>(a.stats_pre + 2 * row) = make_float2(mean, rstd);
         normalise(x, mean, rstd, a.w_pre, w2, a.b_pre, b2);
 #pragma unroll
-        for (int u = 0; u < ITER; ++u) store_piece<DT, TPR, WHOLE>(x[u], a.H, at, u, t, H);
+        for (int u = 0; u < ITER; ++u) store_piece<DT, TPR, HOW>(x[u], a.H, at, u, t, H);
     }
 }
 
@@ -282,7 +304,7 @@ struct Backward {
 constexpr int kBackTeams = 4;  // wavefronts of a workgroup where a row is one's (their sums meet before they leave it)
 
 // SIMPLE: BERT's form, N_pre without a gate (no F, and two sums).
-template <int DT, int TPR, int ITER, bool WHOLE, bool SIMPLE>
+template <int DT, int TPR, int ITER, int HOW, bool SIMPLE>
 __global__ __launch_bounds__(TPR == 64 ? 64 * kBackTeams : TPR) void block_norm_back_kernel(Backward a) {
     constexpr int kTeams = TPR == 64 ? kBackTeams : 1;
     __shared__ float red[TPR > 64 ? 4 * (TPR / 64) : 1];
@@ -301,7 +323,7 @@ __global__ __launch_bounds__(TPR == 64 ? 64 * kBackTeams : TPR) void block_norm_
     };
 #pragma unroll
     for (int i = 0; i < kSums; ++i) clear(i);
-    using Piece = Raw<DT, TPR, WHOLE>;
+    using Piece = Raw<DT, TPR, HOW>;
     Piece w2[ITER];
     if (pre && a.w_pre)
 #pragma unroll
@@ -362,7 +384,7 @@ __global__ __launch_bounds__(TPR == 64 ? 64 * kBackTeams : TPR) void block_norm_
                 float x[kVec];
 #pragma unroll
                 for (int j = 0; j < kVec; ++j) x[j] = a.x_scale * d[u][j];
-                store_piece<DT, TPR, WHOLE>(x, a.dX, at, u, t, H);
+                store_piece<DT, TPR, HOW>(x, a.dX, at, u, t, H);
             }
         if constexpr (!SIMPLE) {
             float s[2] = {0.0f, 0.0f};
@@ -374,7 +396,7 @@ __global__ __launch_bounds__(TPR == 64 ? 64 * kBackTeams : TPR) void block_norm_
                 if (post && a.b_post) b.load(a.b_post, 0, u, t, H);
 #pragma unroll
                 for (int j = 0; j < kVec; ++j) {
-                    if (column<TPR, WHOLE>(u, j, t) >= H) {
+                    if (column<TPR, HOW>(u, j, t) >= H) {
                         d[u][j] = 0.0f;
                         continue;
                     }
@@ -408,7 +430,7 @@ __global__ __launch_bounds__(TPR == 64 ? 64 * kBackTeams : TPR) void block_norm_
         }
         if (a.dF)
 #pragma unroll
-            for (int u = 0; u < ITER; ++u) store_piece<DT, TPR, WHOLE>(d[u], a.dF, at, u, t, H);
+            for (int u = 0; u < ITER; ++u) store_piece<DT, TPR, HOW>(d[u], a.dF, at, u, t, H);
     };
 
     // The rows of this team, one loop for both ways they are dealt (the kernel's code is what a short call waits for): every kTeams-th row of a
@@ -448,7 +470,7 @@ __global__ __launch_bounds__(TPR == 64 ? 64 * kBackTeams : TPR) void block_norm_
         if (whole && end) {
             if (a.dgate)
 #pragma unroll
-                for (int u = 0; u < ITER; ++u) store_piece<BSP_F32, TPR, WHOLE>(acc[kDgate][u], a.dgate, at_group * H, u, t, H);
+                for (int u = 0; u < ITER; ++u) store_piece<BSP_F32, TPR, HOW>(acc[kDgate][u], a.dgate, at_group * H, u, t, H);
             clear(kDgate);
         }
     }
@@ -473,7 +495,7 @@ __global__ __launch_bounds__(TPR == 64 ? 64 * kBackTeams : TPR) void block_norm_
 #pragma unroll
                         for (int j = 0; j < kVec; ++j) v[j] += share[(o * kVec + j) * TPR + t];
             }
-            if (!team) store_piece<BSP_F32, TPR, WHOLE>(v, out, 0, u, t, H);
+            if (!team) store_piece<BSP_F32, TPR, HOW>(v, out, 0, u, t, H);
         }
     });
 }
@@ -545,26 +567,31 @@ int check(int64_t T, int64_t H, int dt, int norms, int kind, const void *gate, i
     return BSP_OK;
 }
 
-template <int DT, int TPR, int ITER>
-void launch_forward(const Forward &a, hipStream_t s) {
-    constexpr int kTeams = TPR < 256 ? 256 / TPR : 1;
-    const int64_t wgs = (a.T + kTeams - 1) / kTeams, most = (int64_t)1 << 20;  // (a launch has less than 2^32 threads along x)
-    const dim3 grid((unsigned)(wgs < most ? wgs : most), (unsigned)((wgs + most - 1) / most));
-    if (a.width % kVec == 0) block_norm_kernel<DT, TPR, ITER, true><<<grid, TPR < 256 ? 256 : TPR, 0, s>>>(a);
-    else block_norm_kernel<DT, TPR, ITER, false><<<grid, TPR < 256 ? 256 : TPR, 0, s>>>(a);
+// f(how).  words: whether the rows and vectors are at addresses of 32-bit words, and (16 bits) the rows of whole ones.
+template <int DT, bool FORWARD, typename F>
+void how_of(int64_t width, bool words, F f) {
+    constexpr bool kNarrow = DT != BSP_F32;
+    if (width % kVec == 0 && (!FORWARD || words)) f(std::integral_constant<int, FORWARD ? kWords : kWhole>{});
+    else if (kNarrow && words) f(std::integral_constant<int, kNarrow ? kWords : kApart>{});
+    else f(std::integral_constant<int, kApart>{});
 }
 
 template <int DT, int TPR, int ITER>
-void launch_backward(const Backward &a, unsigned grid, hipStream_t s) {
+void launch_forward(const Forward &a, bool words, hipStream_t s) {
+    constexpr int kTeams = TPR < 256 ? 256 / TPR : 1;
+    const int64_t wgs = (a.T + kTeams - 1) / kTeams, most = (int64_t)1 << 20;  // (a launch has less than 2^32 threads along x)
+    const dim3 grid((unsigned)(wgs < most ? wgs : most), (unsigned)((wgs + most - 1) / most));
+    how_of<DT, true>(a.width, words, [&](auto how) { block_norm_kernel<DT, TPR, ITER, decltype(how)::value><<<grid, TPR < 256 ? 256 : TPR, 0, s>>>(a); });
+}
+
+template <int DT, int TPR, int ITER>
+void launch_backward(const Backward &a, bool words, unsigned grid, hipStream_t s) {
     constexpr int kThreads = TPR == 64 ? 64 * kBackTeams : TPR;
     const bool simple = a.norms == BSP_NORM_PRE && !a.gate;
-    if (a.width % kVec == 0) {
-        if (simple) block_norm_back_kernel<DT, TPR, ITER, true, true><<<grid, kThreads, 0, s>>>(a);
-        else block_norm_back_kernel<DT, TPR, ITER, true, false><<<grid, kThreads, 0, s>>>(a);
-    } else {
-        if (simple) block_norm_back_kernel<DT, TPR, ITER, false, true><<<grid, kThreads, 0, s>>>(a);
-        else block_norm_back_kernel<DT, TPR, ITER, false, false><<<grid, kThreads, 0, s>>>(a);
-    }
+    how_of<DT, false>(a.width, words, [&](auto how) {
+        if (simple) block_norm_back_kernel<DT, TPR, ITER, decltype(how)::value, true><<<grid, kThreads, 0, s>>>(a);
+        else block_norm_back_kernel<DT, TPR, ITER, decltype(how)::value, false><<<grid, kThreads, 0, s>>>(a);
+    });
 }
 
 }  // namespace
@@ -580,18 +607,21 @@ extern "C" int bsp_block_norm(const void *X, const void *F, int dt, int64_t T, i
     if (T == 0) return BSP_OK;
     if (!X || (!F && (post || gate)) || (pre && !Hn) || (!Z && !pre)) return BSP_ERR_NULL;
     const size_t size = dtype_size(dt);
-    for (const void *p : {X, F, gate, w_post, b_post, w_pre, b_pre, (const void *)Z, (const void *)Hn})
+    bool words = H % 2 == 0;
+    for (const void *p : {X, F, gate, w_post, b_post, w_pre, b_pre, (const void *)Z, (const void *)Hn}) {
         if (!aligned(p, size)) return BSP_ERR_SHAPE;
+        words &= aligned(p, 4);
+    }
     if (!aligned(stats_post, 8) || !aligned(stats_pre, 8)) return BSP_ERR_SHAPE;
     const Forward a = {X, F, gate, w_post, b_post, w_pre, b_pre, Z, Hn, stats_post, stats_pre,
                        T, gate ? T / gate_rows : T, x_scale, eps, (int32_t)H, kind == BSP_NORM_RMS, norms};
     hipStream_t s = (hipStream_t)stream;
     BSP_DISPATCH_DTYPE(dt, DT, {
-        if (H <= 512) launch_forward<DT, 64, 1>(a, s);
-        else if (H <= 1024) launch_forward<DT, 64, 2>(a, s);
-        else if (H <= 2048) launch_forward<DT, 64, 4>(a, s);
-        else if (H <= 4096) launch_forward<DT, 256, 2>(a, s);
-        else launch_forward<DT, 256, 4>(a, s);
+        if (H <= 512) launch_forward<DT, 64, 1>(a, words, s);
+        else if (H <= 1024) launch_forward<DT, 64, 2>(a, words, s);
+        else if (H <= 2048) launch_forward<DT, 64, 4>(a, words, s);
+        else if (H <= 4096) launch_forward<DT, 256, 2>(a, words, s);
+        else launch_forward<DT, 256, 4>(a, words, s);
     });
     return check_launch();
 }
@@ -614,8 +644,11 @@ extern "C" int bsp_block_norm_backward(const void *dZ, const void *dH, const voi
     if ((pre && T && (!dH || !Z || !stats_pre)) || (post && T && (!F || !stats_post)) || (dgate && T && !F)) return BSP_ERR_NULL;
     if (!pre && !dZ && T) return BSP_ERR_NULL;
     const size_t size = dtype_size(dt);
-    for (const void *p : {dZ, dH, Z, F, gate, w_post, b_post, w_pre, (const void *)dX, (const void *)dF})
+    bool words = H % 2 == 0;
+    for (const void *p : {dZ, dH, Z, F, gate, w_post, b_post, w_pre, (const void *)dX, (const void *)dF}) {
         if (!aligned(p, size)) return BSP_ERR_SHAPE;
+        words &= aligned(p, 4);
+    }
     for (const float *p : {stats_post, stats_pre})
         if (!aligned(p, 8)) return BSP_ERR_SHAPE;
     for (const float *p : {(const float *)dw_post, (const float *)db_post, (const float *)dw_pre, (const float *)db_pre, (const float *)dgate})
@@ -638,11 +671,11 @@ extern "C" int bsp_block_norm_backward(const void *dZ, const void *dH, const voi
         for (int i = 0; i < kSums; ++i)
             if (c.out[i] && !(direct && i == kDgate)) a.want |= 1u << i;
         BSP_DISPATCH_DTYPE(dt, DT, {
-            if (H <= 512) launch_backward<DT, 64, 1>(a, (unsigned)d.wgs, s);
-            else if (H <= 1024) launch_backward<DT, 64, 2>(a, (unsigned)d.wgs, s);
-            else if (H <= 2048) launch_backward<DT, 256, 1>(a, (unsigned)d.wgs, s);
-            else if (H <= 4096) launch_backward<DT, 256, 2>(a, (unsigned)d.wgs, s);
-            else launch_backward<DT, 512, 2>(a, (unsigned)d.wgs, s);
+            if (H <= 512) launch_backward<DT, 64, 1>(a, words, (unsigned)d.wgs, s);
+            else if (H <= 1024) launch_backward<DT, 64, 2>(a, words, (unsigned)d.wgs, s);
+            else if (H <= 2048) launch_backward<DT, 256, 1>(a, words, (unsigned)d.wgs, s);
+            else if (H <= 4096) launch_backward<DT, 256, 2>(a, words, (unsigned)d.wgs, s);
+            else launch_backward<DT, 512, 2>(a, words, (unsigned)d.wgs, s);
         });
         if (int st = check_launch()) return st;
     }
