@@ -529,7 +529,10 @@ __global__ __launch_bounds__(64 * kParts) void block_norm_columns_kernel(Columns
     out[(int64_t)(kind == kDgate ? row - kDgate : 0) * a.width + c] = s;
 }
 
-constexpr int64_t kRanges = 512;  // workgroups of the backward pass, at most where the gate's rows allow it
+// Workgroups of the backward pass, at most where the gate's rows allow it.  Two for a compute unit; one where they are of 512 threads (us, 2048 x 8192
+// in bf16, BERT's form 38.5, with two 45, both norms and a gate 74, 87), and where they would have a row or two each, because each has sums to write and
+// to be read again (512 x 4096 15.2, 19.3, both norms and a gate in fp32 25.5, 33.6; but 2048 x 2048 28.4, 27.1).
+int64_t ranges_of(int64_t T, int64_t H) { return H > 4096 || (H > 1024 && T <= 1024) ? 256 : 512; }
 
 // Workgroups, and how the rows are dealt to them.
 struct Deal {
@@ -542,7 +545,8 @@ Deal deal(int64_t T, int64_t H, int64_t gate_rows) {
     const int64_t teams = H <= 1024 ? kBackTeams : 1;
     d.groups = (int32_t)(gate_rows > 0 ? gate_rows : 1);
     d.rows_per_gate = T / d.groups;
-    int64_t rows = (T + kRanges - 1) / kRanges;
+    const int64_t ranges = ranges_of(T, H);
+    int64_t rows = (T + ranges - 1) / ranges;
     rows = (rows + teams - 1) / teams * teams;
     if (d.rows_per_gate >= rows || d.groups == 1) {
         d.pieces = (int32_t)((d.rows_per_gate + rows - 1) / rows);
