@@ -9,7 +9,8 @@
 // Bound by memory.  Row segments alone: 16 lanes to a segment.  Else a workgroup reads a 128 x 128 tile once, 4 x 8 values per thread, and has
 // from it the row segments, the column segments (the rows of the transposed matrix) or the block, and the codes of either
 // orientation; the transposed ones go through LDS.  Measured (MI355X, bf16, us): 16384 x 4096 by rows 33 (6.0 TB/s), 8192 x 1024 7.3; in both
-// orientations 8192 x 4096 by rows 30 to 34 (4.2 TB/s), in blocks 28.5; 64 x 1024 by rows 2.5.
+// orientations 8192 x 4096 by rows 28 to 31 (4.4 TB/s), in blocks 23; 64 x 1024 by rows 2.5.  A width that is no multiple of 8 costs 10 to 25 % (loads
+// that cross lines).
 #include "bsp_common.h"
 #include "bsp_fp8_device.h"
 

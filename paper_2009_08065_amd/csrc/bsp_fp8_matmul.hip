@@ -18,7 +18,7 @@
 // the operand reads of 16 lanes meet all banks.
 //
 // Measured (MI355X, us): 16384 x 4096, K = 4096 225 to 235 (2.4 PFLOP/s), 8192 x 4096, K = 1024 44 (1.6), with GELU 55, 8192 x 1024, K = 4096 37
-// (1.9); in fp32 4096 x 4096, K = 8192 206 (1.3 PFLOP/s), 1024 x 4096, K = 8192 71 (1.0); one token, 4096 x 1024 4.1 with its quantisation.
+// (1.9); in fp32 4096 x 4096, K = 8192 200 (1.4 PFLOP/s), 1024 x 4096, K = 8192 67 (1.0); one token, 4096 x 1024 4.1 with its quantisation.
 // What bounds the large ones: of 231 us in tiles of 256 x 256 182 are left without the loads (the matrix cores at the clock that their power leaves), 210
 // without the LDS reads; tiles of 128 x 128 fall from 266 to 162 without the loads, 16 TB/s of them.  Halves of steps in a ring of four, read into
 // registers ahead of the barrier, took 250, the first half of
