@@ -109,6 +109,22 @@ def test_matmul(dtype, T, M, K):
         assert torch.equal(y, bsp.bsp_matmul_fp8(A, B, out_dtype=dt))
 
 
+@pytest.mark.parametrize("T,M,K", [(70, 2900, 300), (450, 2000, 640), (2000, 66, 500), (65, 65, 70), (1100, 1300, 200)])
+def test_matmul_tiles_that_no_eight_share_evenly(T, M, K):
+    a, b = rand(T + K, T, K), rand(M + K + 1, M, K, std=0.05)
+    A, B = bsp.bsp_fp8_quant(a.cuda())[0], bsp.bsp_fp8_quant(b.cuda(), bsp.FP8_BLOCK)[0]
+    av, bv = orc.value(*orc.quant(a.to(D), False), K, False), orc.value(*orc.quant(b.to(D), True), K, True)
+    want = av @ bv.t()
+    for dt in (torch.bfloat16, torch.float32):
+        bound = fp8_bound(av, bv, dt)
+        y = torch.full((T, M), math.nan, dtype=dt, device="cuda")
+        inside(bsp.bsp_matmul_fp8(A, B, Y=y), want, half(dt) * (want.abs() + bound) + bound)
+        r = rand(7, T, M, dt=dt).cuda()
+        both = want + r.cpu().to(D)
+        mine = r.clone()                             # the residual's place is the result's
+        inside(bsp.bsp_matmul_fp8(A, B, residual=mine, Y=mine), both, half(dt) * (both.abs() + bound) + bound + U * want.abs())
+
+
 @pytest.mark.parametrize("T,M", [(3500, 3600), (4100, 2900)])
 def test_matmul_large_tiles(T, M):
     """Sizes of the largest tile, ragged in both directions; rows and columns at the borders of tiles among those compared."""
@@ -289,6 +305,15 @@ def test_block_norm_widths(dtype, H):
     for T in (1, 5, 67):
         check_norm(T, H, DT[dtype], False, True, True, 1)
     check_norm(6, H, DT[dtype], True, False, True, 0, x_scale=1.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("H", [2, 10, 266, 514, 1030, 2054, 4102, 8190])
+def test_block_norm_rows_of_whole_words(dtype, H):
+    """Even widths that are no multiple of 8: pieces that end with the row, at addresses of words and (unaligned) of half ones."""
+    for aligned in (True, False):
+        check_norm(37, H, DT[dtype], False, True, True, 37, aligned=aligned)
+        check_norm(300, H, DT[dtype], True, False, True, 0, aligned=aligned)
 
 
 @pytest.mark.parametrize("rms", [False, True])
@@ -483,6 +508,27 @@ def test_adamw_8bit(gdtype, unaligned):
             if up:
                 assert (gq[x.reshape(-1) > 0] > 0).all()
         assert torch.equal(copies[i], Wd[i].half())
+
+
+@pytest.mark.parametrize("N", [1, 2, 3, 5, 142, 147, 766])
+def test_adamw_8bit_masks_of_any_width(N):
+    """The mask zeroes weights and leaves moments alone, the factors are an addition to the gradient (one rounding): bit for bit what the step without
+    them gives on that gradient, where rows end anywhere among four elements."""
+    M, R, lam = 48, 16, 1e-3
+    w, g = rand(N, M, N, std=0.05), rand(N + 1, M, N, std=1e-3)
+    gen = torch.Generator().manual_seed(N)
+    keep, alpha = (torch.rand(M // R, N, generator=gen) < 0.5).to(torch.uint8), torch.rand(M // R, N, generator=gen)
+    factor = (torch.tensor(lam) * alpha).repeat_interleave(R, 0)
+    added = (factor.to(D) * w.to(D) + g.to(D)).float()
+    runs = []
+    for grad, more in ((g, dict(keep=[keep.cuda()], alpha=[alpha.cuda()], lam=lam, R=R)), (added, {})):
+        W, copies = [w.cuda()], [torch.empty(M, N, dtype=torch.bfloat16, device="cuda")]
+        m, v, s = bsp.bsp_adamw_state(W, 8)
+        bsp.bsp_adamw_step(W, [grad.cuda()], m, v, 1e-3, t=1, scales=s, weight_decay=0.01, seed=3, copies=copies, **more, **HYPER)
+        runs.append((W[0].cpu(), m[0].view(torch.uint8).cpu(), v[0].view(torch.uint8).cpu(), s[0].cpu(), copies[0].cpu()))
+    kept = keep.repeat_interleave(R, 0).bool()
+    assert torch.equal(runs[0][0], torch.where(kept, runs[1][0], torch.zeros(()))) and torch.equal(runs[0][4], runs[0][0].bfloat16())
+    assert all(torch.equal(a, b) for a, b in zip(runs[0][1:4], runs[1][1:4]))
 
 
 def test_adamw_8bit_moments_follow_over_steps():
