@@ -308,7 +308,8 @@ template <int DT, int TPR, int ITER, int HOW, bool SIMPLE>
 __global__ __launch_bounds__(TPR == 64 ? 64 * kBackTeams : TPR) void block_norm_back_kernel(Backward a) {
     constexpr int kTeams = TPR == 64 ? kBackTeams : 1;
     __shared__ float red[TPR > 64 ? 4 * (TPR / 64) : 1];
-    __shared__ float share[kTeams > 1 ? (kTeams - 1) * TPR * kVec : 1];
+    constexpr int kColumns = TPR * ITER * kVec;
+    __shared__ __align__(16) float share[kTeams > 1 ? 2 * kTeams * kColumns : 4];
     int turn = 0;
     const int t = threadIdx.x % TPR, team = threadIdx.x / TPR, H = a.width;
     const bool pre = SIMPLE || (a.norms & BSP_NORM_PRE), post = !SIMPLE && (a.norms & BSP_NORM_POST);
@@ -474,28 +475,30 @@ __global__ __launch_bounds__(TPR == 64 ? 64 * kBackTeams : TPR) void block_norm_
             clear(kDgate);
         }
     }
-    // the workgroup's sums: the teams' in ascending order, a piece at a time through LDS
+    // the workgroup's sums: the teams' by columns in LDS, each thread adds up some columns' in ascending order
+    int half = 0;
     static_for<0, kSums>([&](auto kind) {
         constexpr int i = decltype(kind)::value;
         if (SIMPLE && i != kDwPre && i != kDbPre) return;
         if (!((a.want >> i) & 1u)) return;  // uniform
         float *out = a.sums + ((int64_t)i * gridDim.x + blockIdx.x) * H;
+        if constexpr (kTeams > 1) {
+            float *mine = share + (half * kTeams + team) * kColumns, *first = share + half * kTeams * kColumns;
+            half ^= 1;  // (the other half is read no more: everybody has passed the barrier of the kind before)
 #pragma unroll
-        for (int u = 0; u < ITER; ++u) {
-            float(&v)[kVec] = acc[i][u];
-            if constexpr (kTeams > 1) {
-                __syncthreads();
-                if (team)
+            for (int u = 0; u < ITER; ++u)
 #pragma unroll
-                    for (int j = 0; j < kVec; ++j) share[((team - 1) * kVec + j) * TPR + t] = v[j];
-                __syncthreads();
-                if (!team)
+                for (int j = 0; j < kVec; ++j) mine[column<TPR, HOW>(u, j, t)] = acc[i][u][j];
+            __syncthreads();
+            for (int c = threadIdx.x; c < H; c += TPR * kTeams) {
+                float s = first[c];
 #pragma unroll
-                    for (int o = 0; o < kTeams - 1; ++o)
-#pragma unroll
-                        for (int j = 0; j < kVec; ++j) v[j] += share[(o * kVec + j) * TPR + t];
+                for (int o = 1; o < kTeams; ++o) s += first[o * kColumns + c];
+                out[c] = s;
             }
-            if (!team) store_piece<BSP_F32, TPR, HOW>(v, out, 0, u, t, H);
+        } else {
+#pragma unroll
+            for (int u = 0; u < ITER; ++u) store_piece<BSP_F32, TPR, HOW>(acc[i][u], out, 0, u, t, H);
         }
     });
 }
