@@ -38,7 +38,7 @@ def build_host():
     subprocess.run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-fvisibility=hidden", "-I", INCLUDE,
                     "-isystem", os.path.join(torch_dir, "include"), "-isystem", sysconfig.get_paths()["include"],
                     os.path.join(CSRC, "bsp_host.cpp"), "-o", HOST_LIB, "-L", os.path.join(torch_dir, "lib"),
-                    "-ltorch_python", "-ltorch_cpu", "-lc10", "-L", HERE, "-l:libbsp.so", "-Wl,-rpath,$ORIGIN"], check=True)
+                    "-ltorch_python", "-ltorch_cpu", "-ltorch_hip", "-lc10", "-L", HERE, "-l:libbsp.so", "-Wl,-rpath,$ORIGIN"], check=True)
 
 
 def _inputs():

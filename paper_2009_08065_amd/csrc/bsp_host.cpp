@@ -13,6 +13,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <ATen/core/Tensor.h>
+#include <ATen/hip/EmptyTensor.h>
 #include <ATen/ops/empty.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -465,7 +466,8 @@ struct RowArgs {
                                                                                                                             : fail("stats must be float32 [T, 2]");
     }
     int type() const { return like->scalar_type() == at::kFloat ? BSP_F32 : (like->scalar_type() == at::kBFloat16 ? BSP_BF16 : BSP_F16); }
-    at::Tensor make(at::IntArrayRef size, at::ScalarType t) const { return at::empty(size, at::TensorOptions().dtype(t).device(like->device())); }
+    // (what at::empty comes to on a GPU, without its way there)
+    at::Tensor make(at::IntArrayRef size, at::ScalarType t) const { return at::Tensor(at::detail::empty_cuda(size, t, like->device(), c10::nullopt)); }
 };
 
 void *address(const at::Tensor *t) { return t ? t->data_ptr() : nullptr; }
