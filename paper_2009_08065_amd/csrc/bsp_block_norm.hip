@@ -6,7 +6,7 @@
 // Both are bound by memory: forward reads X and F and writes Z and H, backward reads up to dZ, dH, Z and F and writes dX and dF.  So
 // a row stays in the registers of its team of threads from the first load to the last store: statistics, both norms and the rounding
 // between them (N_pre reads Z as it is stored, which is what the backward pass will see) cost no second look at memory.
-// A team is one wavefront while a row has no more than 32 values for a lane (backward 16), else a workgroup.
+// A team is 16 lanes for the narrowest rows, one wavefront while a row has no more than 32 values for a lane (backward 16), else a workgroup.
 // Measured (MI355X, us, of a pass among others): forward 8192 x 1024 in bf16, BERT's form 14.3 (4.7 TB/s), both norms and a gate 16; in fp32 23.0 (5.8
 // TB/s); 16384 x 4096 in bf16 95 (5.6).  Backward 8192 x 1024, BERT's form 21 (17.4 and 4.1 for the columns; 4.0 TB/s), both norms and a gate 32; 16384 x
 // 4096 143 (4.7 TB/s) and 187.
@@ -66,13 +66,24 @@ struct Raw {
 #pragma unroll
             for (int i = 0; i < (int)(sizeof(d) / 16); ++i) d[i] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(row, c + 16 * i, 0, 0));
         } else {
-            const __amdgpu_buffer_rsrc_t row = buffer_of_row<size>(p, at, H);
             uint32_t w[8];
+            if constexpr (TPR < 64) {  // (several rows in a wavefront: the last column in the place of those past it, and zeros after that)
 #pragma unroll
-            for (int j = 0; j < kVec; ++j) {
-                const int c = size * column<TPR, HOW>(u, j, t);
-                if constexpr (DT == BSP_F32) w[j] = __builtin_amdgcn_raw_buffer_load_b32(row, c, 0, 0);
-                else w[j] = __builtin_amdgcn_raw_buffer_load_b16(row, c, 0, 0);
+                for (int j = 0; j < kVec; ++j) {
+                    const int c = column<TPR, HOW>(u, j, t);
+                    if constexpr (DT == BSP_F32) w[j] = ((const uint32_t *)p)[at + (c < H ? c : H - 1)];
+                    else w[j] = ((const uint16_t *)p)[at + (c < H ? c : H - 1)];
+                }
+#pragma unroll
+                for (int j = 0; j < kVec; ++j) w[j] = column<TPR, HOW>(u, j, t) < H ? w[j] : 0u;
+            } else {
+                const __amdgpu_buffer_rsrc_t row = buffer_of_row<size>(p, at, H);
+#pragma unroll
+                for (int j = 0; j < kVec; ++j) {
+                    const int c = size * column<TPR, HOW>(u, j, t);
+                    if constexpr (DT == BSP_F32) w[j] = __builtin_amdgcn_raw_buffer_load_b32(row, c, 0, 0);
+                    else w[j] = __builtin_amdgcn_raw_buffer_load_b16(row, c, 0, 0);
+                }
             }
             if constexpr (DT == BSP_F32) {
                 d[0] = make_uint4(w[0], w[1], w[2], w[3]);
@@ -119,6 +130,10 @@ __device__ __forceinline__ void store_piece(const float (&v)[kVec], void *p, int
         } else {
             __builtin_amdgcn_raw_buffer_store_b128(u32x4{cvt_pk<DT>(v[0], v[1]), cvt_pk<DT>(v[2], v[3]), cvt_pk<DT>(v[4], v[5]), cvt_pk<DT>(v[6], v[7])}, row, c, 0, 0);
         }
+    } else if constexpr (TPR < 64) {
+#pragma unroll
+        for (int j = 0; j < kVec; ++j)
+            if (column<TPR, HOW>(u, j, t) < H) elem<DT>::store(p, at + column<TPR, HOW>(u, j, t), v[j]);
     } else {
         constexpr int size = DT == BSP_F32 ? 4 : 2;
         const __amdgpu_buffer_rsrc_t row = buffer_of_row<size>(p, at, H);
@@ -156,12 +171,20 @@ __device__ __forceinline__ float wave_sum(float x) {
     return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), 63));
 }
 
+// The sum of 16 lanes' values, in every one of them: rotations within the row.
+__device__ __forceinline__ float sum_of_16(float x) {
+    x = add_dpp<0x121, 0xf>(x);
+    x = add_dpp<0x122, 0xf>(x);
+    x = add_dpp<0x124, 0xf>(x);
+    return add_dpp<0x128, 0xf>(x);
+}
+
 // Sums of K values over the TPR threads of a team, in every one of them.  LDS: `red` of 2 * K * TPR / 64 floats, its halves in turn, so that
 // one barrier a sum is enough.
 template <int TPR, int K>
 __device__ __forceinline__ void team_sum(float (&v)[K], float *red, int &turn) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = wave_sum(v[k]);
+    for (int k = 0; k < K; ++k) v[k] = TPR == 16 ? sum_of_16(v[k]) : wave_sum(v[k]);
     if constexpr (TPR > 64) {
         constexpr int W = TPR / 64;
         float *r = red + turn * K * W;
@@ -301,12 +324,18 @@ struct Backward {
     uint32_t want;                                      // bit i: sums of kind i
 };
 
+// Whether a row is for 16 lanes, four of them in a wavefront.  (us, bf16, BERT's form and both norms with a gate: 32768 x 64 forward 7.0 and 8.6, with a
+// wavefront for a row 16.6 and 22.4, backward 11.4 and 16.9, 22.3 and 45; 32768 x 256 13.7 and 15.7, 18.4 and 23, backward 19.4 and 28, 23.4 and 46; 17221
+// x 79 13.0 and 20.4, 24 and 37; but 14904 x 228, which is no multiple of 8, 18.5 and 42, 18.2 and 26.)
+bool of_16(int64_t H) { return H <= 128 || (H <= 256 && H % kVec == 0); }
+
 constexpr int kBackTeams = 4;  // wavefronts of a workgroup where a row is one's (their sums meet before they leave it)
+constexpr int teams_of(int tpr) { return tpr <= 64 ? 64 * kBackTeams / tpr : 1; }
 
 // SIMPLE: BERT's form, N_pre without a gate (no F, and two sums).
 template <int DT, int TPR, int ITER, int HOW, bool SIMPLE>
-__global__ __launch_bounds__(TPR == 64 ? 64 * kBackTeams : TPR) void block_norm_back_kernel(Backward a) {
-    constexpr int kTeams = TPR == 64 ? kBackTeams : 1;
+__global__ __launch_bounds__(TPR * teams_of(TPR)) void block_norm_back_kernel(Backward a) {
+    constexpr int kTeams = teams_of(TPR);
     __shared__ float red[TPR > 64 ? 4 * (TPR / 64) : 1];
     constexpr int kColumns = TPR * ITER * kVec;
     __shared__ __align__(16) float share[kTeams > 1 ? 2 * kTeams * kColumns : 4];
@@ -559,7 +588,7 @@ struct Deal {
 
 Deal deal(int64_t T, int64_t H, int64_t gate_rows) {
     Deal d;
-    const int64_t teams = H <= 1024 ? kBackTeams : 1;
+    const int64_t teams = teams_of(of_16(H) ? 16 : H <= 1024 ? 64 : 256);
     d.groups = (int32_t)(gate_rows > 0 ? gate_rows : 1);
     d.rows_per_gate = T / d.groups;
     const int64_t ranges = ranges_of(T, H);
@@ -589,11 +618,11 @@ int check(int64_t T, int64_t H, int dt, int norms, int kind, const void *gate, i
 }
 
 // f(how).  words: whether the rows and vectors are at addresses of 32-bit words, and (16 bits) the rows of whole ones.
-template <int DT, bool FORWARD, typename F>
+template <int DT, int TPR, bool FORWARD, typename F>
 void how_of(int64_t width, bool words, F f) {
-    constexpr bool kNarrow = DT != BSP_F32;
-    if (width % kVec == 0 && (!FORWARD || words)) f(std::integral_constant<int, FORWARD ? kWords : kWhole>{});
-    else if (kNarrow && words) f(std::integral_constant<int, kNarrow ? kWords : kApart>{});
+    constexpr bool kAlone = TPR >= 64, kNarrow = DT != BSP_F32;  // (buffers are for rows that have a wavefront to themselves)
+    if (width % kVec == 0 && (!FORWARD || !kAlone || words)) f(std::integral_constant<int, FORWARD && kAlone ? kWords : kWhole>{});
+    else if (kAlone && kNarrow && words) f(std::integral_constant<int, kAlone && kNarrow ? kWords : kApart>{});
     else f(std::integral_constant<int, kApart>{});
 }
 
@@ -602,14 +631,14 @@ void launch_forward(const Forward &a, bool words, hipStream_t s) {
     constexpr int kTeams = TPR < 256 ? 256 / TPR : 1;
     const int64_t wgs = (a.T + kTeams - 1) / kTeams, most = (int64_t)1 << 20;  // (a launch has less than 2^32 threads along x)
     const dim3 grid((unsigned)(wgs < most ? wgs : most), (unsigned)((wgs + most - 1) / most));
-    how_of<DT, true>(a.width, words, [&](auto how) { block_norm_kernel<DT, TPR, ITER, decltype(how)::value><<<grid, TPR < 256 ? 256 : TPR, 0, s>>>(a); });
+    how_of<DT, TPR, true>(a.width, words, [&](auto how) { block_norm_kernel<DT, TPR, ITER, decltype(how)::value><<<grid, TPR < 256 ? 256 : TPR, 0, s>>>(a); });
 }
 
 template <int DT, int TPR, int ITER>
 void launch_backward(const Backward &a, bool words, unsigned grid, hipStream_t s) {
-    constexpr int kThreads = TPR == 64 ? 64 * kBackTeams : TPR;
+    constexpr int kThreads = TPR * teams_of(TPR);
     const bool simple = a.norms == BSP_NORM_PRE && !a.gate;
-    how_of<DT, false>(a.width, words, [&](auto how) {
+    how_of<DT, TPR, false>(a.width, words, [&](auto how) {
         if (simple) block_norm_back_kernel<DT, TPR, ITER, decltype(how)::value, true><<<grid, kThreads, 0, s>>>(a);
         else block_norm_back_kernel<DT, TPR, ITER, decltype(how)::value, false><<<grid, kThreads, 0, s>>>(a);
     });
@@ -638,7 +667,9 @@ extern "C" int bsp_block_norm(const void *X, const void *F, int dt, int64_t T, i
                        T, gate ? T / gate_rows : T, x_scale, eps, (int32_t)H, kind == BSP_NORM_RMS, norms};
     hipStream_t s = (hipStream_t)stream;
     BSP_DISPATCH_DTYPE(dt, DT, {
-        if (H <= 512) launch_forward<DT, 64, 1>(a, words, s);
+        if (H <= 128) launch_forward<DT, 16, 1>(a, words, s);
+        else if (of_16(H)) launch_forward<DT, 16, 2>(a, words, s);
+        else if (H <= 512) launch_forward<DT, 64, 1>(a, words, s);
         else if (H <= 1024) launch_forward<DT, 64, 2>(a, words, s);
         else if (H <= 2048) launch_forward<DT, 64, 4>(a, words, s);
         else if (H <= 4096) launch_forward<DT, 256, 2>(a, words, s);
@@ -692,7 +723,9 @@ extern "C" int bsp_block_norm_backward(const void *dZ, const void *dH, const voi
         for (int i = 0; i < kSums; ++i)
             if (c.out[i] && !(direct && i == kDgate)) a.want |= 1u << i;
         BSP_DISPATCH_DTYPE(dt, DT, {
-            if (H <= 512) launch_backward<DT, 64, 1>(a, words, (unsigned)d.wgs, s);
+            if (H <= 128) launch_backward<DT, 16, 1>(a, words, (unsigned)d.wgs, s);
+            else if (of_16(H)) launch_backward<DT, 16, 2>(a, words, (unsigned)d.wgs, s);
+            else if (H <= 512) launch_backward<DT, 64, 1>(a, words, (unsigned)d.wgs, s);
             else if (H <= 1024) launch_backward<DT, 64, 2>(a, words, (unsigned)d.wgs, s);
             else if (H <= 2048) launch_backward<DT, 256, 1>(a, words, (unsigned)d.wgs, s);
             else if (H <= 4096) launch_backward<DT, 256, 2>(a, words, (unsigned)d.wgs, s);

@@ -307,6 +307,16 @@ def test_block_norm_widths(dtype, H):
     check_norm(6, H, DT[dtype], True, False, True, 0, x_scale=1.0)
 
 
+@pytest.mark.parametrize("H", [1, 5, 8, 79, 96, 128, 129, 200, 248, 256, 257])
+def test_block_norm_narrow_rows(H):
+    """Several rows in a wavefront: the last ones missing, gate rows of one token and of many, rows at any address."""
+    for dt in (torch.float32, torch.bfloat16):
+        check_norm(1, H, dt, False, True, True, 1)
+        check_norm(15, H, dt, True, True, False, 5, aligned=False)
+        check_norm(1030, H, dt, False, True, True, 515)
+        check_norm(3 * 700, H, dt, False, False, True, 3)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("H", [2, 10, 266, 514, 1030, 2054, 4102, 8190])
 def test_block_norm_rows_of_whole_words(dtype, H):
