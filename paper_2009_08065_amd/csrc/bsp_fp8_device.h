@@ -106,9 +106,16 @@ __device__ __forceinline__ void finish8(float (&v)[8], const float (&bias)[8], i
             __builtin_memcpy(o, &x, 16);
         }
     } else {
+        if (residual) {  // all loads before the first store: a load waits for the stores before it, and seven of them in turn took 25 us where rows end here
+            float x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = elem<DT>::load(r, k < cols ? k : 0);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] += x[k];
+        }
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            if (k < cols) elem<DT>::store(o, k, residual ? v[k] + elem<DT>::load(r, k) : v[k]);
+            if (k < cols) elem<DT>::store(o, k, v[k]);
     }
 }
 
