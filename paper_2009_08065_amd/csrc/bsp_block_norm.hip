@@ -8,7 +8,7 @@
 // between them (N_pre reads Z as it is stored, which is what the backward pass will see) cost no second look at memory.
 // A team is 16 lanes for the narrowest rows, one wavefront while a row has no more than 32 values for a lane (backward 16), else a workgroup.
 // Measured (MI355X, us, of a pass among others): forward 8192 x 1024 in bf16, BERT's form 14.3 (4.7 TB/s), both norms and a gate 16; in fp32 23.0 (5.8
-// TB/s); 16384 x 4096 in bf16 95 (5.6).  Backward 8192 x 1024, BERT's form 21 (17.4 and 4.1 for the columns; 4.0 TB/s), both norms and a gate 32; 16384 x
+// TB/s); 16384 x 4096 in bf16 95 (5.6).  Backward 8192 x 1024, BERT's form 19.6 to 20.3 (16.9 and 3.9 for the columns; 4.2 TB/s), both norms and a gate 30; 16384 x
 // 4096 143 (4.7 TB/s) and 187.
 // Sums are fp32: of a row by the lanes and then across them; the mean first, then the squares of what is left, which a
 // sum of squares less the square of the sum would lose where the mean is large.  The sums down the columns (gradients of w, b and gate) are kept
