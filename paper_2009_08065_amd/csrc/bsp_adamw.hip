@@ -439,7 +439,7 @@ extern "C" int bsp_adamw_step(const bsp_adamw_tensor *tensors, int64_t count, in
     if (!valid_dtype(gdt) || (cdt != BSP_BF16 && cdt != BSP_F16)) return BSP_ERR_DTYPE;
     if (!lr_t && t < 1) return BSP_ERR_SHAPE;
     const int64_t largest = state_bits == 32 ? kThreads * 4 : 4 * kChunk8;
-    int64_t all = 0;
+    int64_t all = 0, most = 0;
     for (int64_t i = 0; i < count; ++i) {  // all of them before the first launch
         const bsp_adamw_tensor &x = tensors[i];
         if (x.M < 0 || x.N < 0 || x.N > 0x7fffffff || (x.M && x.N > 0x7fffffffffffll / x.M)) return BSP_ERR_SHAPE;
@@ -449,12 +449,14 @@ extern "C" int bsp_adamw_step(const bsp_adamw_tensor *tensors, int64_t count, in
         const int64_t n = (x.M * x.N + largest - 1) / largest;
         if (n >= kMostWorkgroups) return BSP_ERR_SHAPE;
         all += n;
+        most = n > most ? n : most;
         if (!aligned(x.w, 4) || !aligned(x.g, dtype_size(gdt)) || (state_bits == 32 && (!aligned(x.m, 4) || !aligned(x.v, 4))) ||
             !aligned(x.scales, 4) || !aligned(x.copy, 2) || !aligned(x.alpha, 4))
             return BSP_ERR_SHAPE;
     }
     if (const int shared = overlapping(tensors, count)) return shared > 0 ? BSP_ERR_SHAPE : BSP_ERR_CAPACITY;
-    const int per = all >= 1024 * ((count + kMaxTensors - 1) / kMaxTensors) ? 4 : (state_bits == 32 ? 2 : 1);
+    // (a tensor beside very many small ones: its part of a launch has to stay below the most there are)
+    const int per = all >= 1024 * ((count + kMaxTensors - 1) / kMaxTensors) || most >= kMostWorkgroups / 4 ? 4 : (state_bits == 32 ? 2 : 1);
     const int64_t chunk = per * (state_bits == 32 ? (int64_t)kThreads : kChunk8);
     Hyper h;
     h.lr = (float)lr;
