@@ -469,7 +469,8 @@ int bsp_block_norm_backward(const void *dZ, const void *dH, const void *Z, const
  * tokens are quantised on the way), 256-byte aligned.
  *
  * residual may be Y; other overlaps of results and operands are not allowed.  rows, T may be 0 (nothing is done); K <= 2^23;
- * launches are of less than 2^32 threads: 2^36 padded elements to quantise, 2^27 rows of B, 2^30 of A are refused.  Errors: BSP_ERR_NULL,
+ * launches are of less than 2^32 threads: 2^36 elements to quantise by rows alone (rows padded to 32, columns to 128), 2^37 in blocks or transposed (both
+ * padded to 128), 2^27 rows of B, 2^30 of A are refused.  Errors: BSP_ERR_NULL,
  * BSP_ERR_DTYPE (types, layout, act), BSP_ERR_SHAPE (sizes, A, B, Q, Qt not 16-byte aligned, others not by their element), BSP_ERR_CAPACITY (ws_bytes too small). */
 typedef enum { BSP_FP8_ROW = 0, BSP_FP8_BLOCK = 1 } bsp_fp8_layout;
 int bsp_fp8_quant(const void *X, int xdt, int64_t rows, int64_t cols, int layout, void *Q, uint8_t *S, void *Qt, uint8_t *St,

@@ -212,7 +212,9 @@ extern "C" int bsp_fp8_quant(const void *X, int xdt, int64_t rows, int64_t cols,
     if (!aligned(X, dtype_size(xdt)) || !aligned(Q, 16) || !aligned(Qt, 16)) return BSP_ERR_SHAPE;
     const int64_t tiles_r = (rows + 127) / 128, tiles_c = (cols + 127) / 128;
     const int64_t rows_grid = tiles_c * ((rows + kRowsEach * 16 - 1) / (kRowsEach * 16));
-    if (rows_grid >= ((int64_t)1 << 24)) return BSP_ERR_SHAPE;  // (a launch has less than 2^32 threads; the other kernel's tiles are four times as large)
+    // a launch has less than 2^32 threads: those of the kernel that runs (up to 64 rows a tile's are the more)
+    const bool by_rows = layout == BSP_FP8_ROW && !Qt;
+    if (by_rows ? rows_grid >= ((int64_t)1 << 32) / kThreads : tiles_r * tiles_c >= ((int64_t)1 << 32) / kTileThreads) return BSP_ERR_SHAPE;
     const Quant a = {X, (uint8_t *)Q, S, (uint8_t *)Qt, St, rows, cols, tiles_c, 128 * tiles_c, 128 * tiles_r};
     BSP_DISPATCH_DTYPE(xdt, DT, { launch<DT>(a, (unsigned)(tiles_r * tiles_c), rows_grid, layout == BSP_FP8_BLOCK, Qt != nullptr, (hipStream_t)stream); });
     return check_launch();

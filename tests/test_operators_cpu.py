@@ -196,3 +196,15 @@ def test_random_rounding_keeps_the_mean():
     for other in (orc.random_bits(n, 4, 11)[0], orc.random_bits(n, 3, 12)[0]):
         assert float((bits == other).double().mean()) < 1e-3
     assert abs(float(bits.double().mean()) / 65535 - 0.5) < 5 * 0.29 / math.sqrt(n)
+
+
+def test_quantisation_of_a_few_very_long_rows_is_refused():
+    """Tiles of 128 x 128 are launched with 512 threads each: 2^23 of them side by side are 2^32 threads, however few the rows; by rows alone a line of up
+    to 32 rows and 128 columns has 256."""
+    q = bsp.lib().bsp_fp8_quant
+    for rows in (1, 32, 64):
+        for cols in (1 << 30, (1 << 30) + 1, (1 << 31) - 1):
+            assert q(P, 1, rows, cols, bsp.FP8_BLOCK, P, P, None, None, None) == SHAPE
+            assert q(P, 1, rows, cols, bsp.FP8_BLOCK, P, P, P, P, None) == SHAPE
+            assert q(P, 1, rows, cols, bsp.FP8_ROW, None, None, P, P, None) == SHAPE
+    assert q(P, 1, 33, 1 << 30, bsp.FP8_ROW, P, P, None, None, None) == SHAPE and q(P, 1, 1, (1 << 31) - 1, bsp.FP8_ROW, P, P, None, None, None) == SHAPE
