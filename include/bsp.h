@@ -192,14 +192,14 @@ int bsp_adam_step(float *W, const void *G, int gdt, float *m, float *v, int64_t 
  *   before they are stored.  All-zero codes and scales are a fresh state.
  * tensors: HOST array of `count` descriptions, read during the call; device pointers in it.  Tensors are [M, N] row-major and
  *   contiguous (a vector: M = 1), of any size, 0 included; keep and alpha are [M / R, N], R is read only with them.
- *   No two tensors of a call may overlap (weights that do, a tied tensor listed twice, are refused).  Addresses need
- *   their element's alignment.
+ *   What a call writes (weights, moments, scales, copies) may not overlap (it is refused: a tied tensor listed twice, say), nor
+ *   may gradients, masks and factors with it; those may be shared.  Addresses need their element's alignment.
  * lr_t: NULL, or two device floats {lr, t} that the kernels read in the place of the arguments: a step that was captured in
  *   a graph is replayed with new ones (t as a float, 1 or more: exact up to 2^24).  A captured step without it repeats its t, and its random bits.
  * Up to 40 tensors are one launch.  Errors: BSP_ERR_NULL, BSP_ERR_DTYPE (gdt; cdt other than bf16 / fp16),
  * BSP_ERR_SHAPE (state_bits, t < 1 without lr_t, negative sizes, N >= 2^31, 2^34 elements or more, M % R != 0 with
  * keep or alpha, misalignment,
- * weights that overlap), BSP_ERR_CAPACITY (no host memory for that check). */
+ * results that overlap), BSP_ERR_CAPACITY (no host memory for that check). */
 typedef struct {
     float *w;
     const void *g;

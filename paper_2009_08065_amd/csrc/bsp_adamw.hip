@@ -402,27 +402,53 @@ void launch(const Table &tab, const Hyper &h, unsigned wgs, int bits, int per, h
     else adamw32_kernel<GDT, CDT, 2><<<wgs, kThreads, 0, s>>>(tab, h);
 }
 
-// Whether two tensors' weights share memory (a tied tensor that is listed twice would be updated by two workgroups at once).
-// 0 no, 1 yes, -1 no memory to find out.  In ascending order, as models allocate them, one look is enough.
-int overlapping(const bsp_adamw_tensor *x, int64_t count) {
-    const float *end = nullptr;
-    bool ascending = true;
-    for (int64_t i = 0; i < count && ascending; ++i) {
-        if (x[i].M == 0 || x[i].N == 0) continue;
-        ascending = x[i].w >= end;
-        end = x[i].w + x[i].M * x[i].N;
+// Whether anything that the step writes shares memory: the same tensor listed twice, say, would be updated by two workgroups at once.
+// 0 no, 1 yes, -1 no memory to find out.  Each kind in ascending order and apart from the others, as models allocate them or cut them out of buffers, is
+// seen in one look; else all are sorted (us on the host, 12 and 288 tensors with copies: 0.25 and 5, sorted 1.2 and 45).
+using Range = std::pair<uintptr_t, uintptr_t>;
+constexpr int kWritten = 5;
+inline Range written(const bsp_adamw_tensor &x, int kind, int bits) {
+    const int64_t n = x.M * x.N;
+    const void *at = nullptr;
+    int64_t bytes = 0;
+    switch (kind) {
+        case 0: at = x.w, bytes = 4 * n; break;
+        case 1: at = x.m, bytes = bits / 8 * n; break;
+        case 2: at = x.v, bytes = bits / 8 * n; break;
+        case 3: at = x.copy, bytes = 2 * n; break;
+        default: at = bits == 8 ? x.scales : nullptr, bytes = (n + kBlock - 1) / kBlock * 8; break;
     }
-    if (ascending) return 0;
-    using Range = std::pair<const float *, const float *>;
-    Range *r = new (std::nothrow) Range[(size_t)count];
-    if (!r) return -1;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(at);
+    return {a, a ? a + (uintptr_t)bytes : a};  // (empty where there is none)
+}
+
+int overlapping(const bsp_adamw_tensor *x, int64_t count, int bits) {
+    Range span[kWritten];
+    bool apart = true;
+    for (int k = 0; k < kWritten; ++k) {
+        span[k] = {0, 0};
+        for (int64_t i = 0; i < count; ++i) {
+            const Range r = written(x[i], k, bits);
+            if (r.first == r.second) continue;
+            if (span[k].second == 0) span[k].first = r.first;
+            apart &= r.first >= span[k].second;
+            span[k].second = r.second;
+        }
+        for (int o = 0; o < k; ++o) apart &= span[o].second <= span[k].first || span[k].second <= span[o].first;
+    }
+    if (apart) return 0;
+    Range *all = new (std::nothrow) Range[(size_t)(kWritten * count)];
+    if (!all) return -1;
     int64_t n = 0;
-    for (int64_t i = 0; i < count; ++i)
-        if (x[i].M && x[i].N) r[n++] = {x[i].w, x[i].w + x[i].M * x[i].N};
-    std::sort(r, r + n);
+    for (int k = 0; k < kWritten; ++k)
+        for (int64_t i = 0; i < count; ++i) {
+            const Range r = written(x[i], k, bits);
+            if (r.first != r.second) all[n++] = r;
+        }
+    std::sort(all, all + n);
     int found = 0;
-    for (int64_t i = 1; i < n; ++i) found |= r[i].first < r[i - 1].second;
-    delete[] r;
+    for (int64_t i = 1; i < n; ++i) found |= all[i].first < all[i - 1].second;
+    delete[] all;
     return found;
 }
 
@@ -454,7 +480,7 @@ extern "C" int bsp_adamw_step(const bsp_adamw_tensor *tensors, int64_t count, in
             !aligned(x.scales, 4) || !aligned(x.copy, 2) || !aligned(x.alpha, 4))
             return BSP_ERR_SHAPE;
     }
-    if (const int shared = overlapping(tensors, count)) return shared > 0 ? BSP_ERR_SHAPE : BSP_ERR_CAPACITY;
+    if (const int shared = overlapping(tensors, count, state_bits)) return shared > 0 ? BSP_ERR_SHAPE : BSP_ERR_CAPACITY;
     // (a tensor beside very many small ones: its part of a launch has to stay below the most there are)
     const int per = all >= 1024 * ((count + kMaxTensors - 1) / kMaxTensors) || most >= kMostWorkgroups / 4 ? 4 : (state_bits == 32 ? 2 : 1);
     const int64_t chunk = per * (state_bits == 32 ? (int64_t)kThreads : kChunk8);

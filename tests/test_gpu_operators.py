@@ -806,3 +806,38 @@ def test_the_layer_captured_with_its_workspace():
             g.replay()
             torch.cuda.synchronize()
             assert torch.equal(y, bsp.bsp_linear_fp8(x, W))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_results_side_by_side_in_one_buffer(bits):
+    """Neighbours that touch are not taken for an overlap, in any order; a copy, a moment or scales listed twice are refused and nothing is written."""
+    shapes = [(16, 16), (1, 300), (3, 171), (48, 16)]
+    W, G, _, _ = adamw_inputs(31, torch.float32, shapes, False)
+    G = on_gpu(G)
+    runs = []
+    for order in (1, -1, 0):                            # one buffer, ascending and descending; tensors of their own
+        w, c, (m, v, s) = on_gpu(W), [torch.zeros_like(x, dtype=torch.bfloat16, device="cuda") for x in W], bsp.bsp_adamw_state(on_gpu(W), bits)
+        if order:
+            lists = [w, m, v, c] + ([s] if s else [])
+            flat = [t for of in zip(*lists) for t in of][::order]
+            buf = torch.empty(sum(-(-t.nbytes // 4) * 4 for t in flat), dtype=torch.uint8, device="cuda")
+            at, new = 0, {}
+            for t in flat:
+                new[id(t)] = buf[at:at + t.nbytes].view(t.dtype).view(t.shape)
+                new[id(t)].copy_(t)
+                at += -(-t.nbytes // 4) * 4
+            w, m, v, c = ([new[id(t)] for t in of] for of in (w, m, v, c))
+            s = [new[id(t)] for t in s] if s else None
+        for t in (1, 2):
+            bsp.bsp_adamw_step(w, G, m, v, 1e-3, t=t, scales=s, copies=c, weight_decay=0.1, seed=2, **HYPER)
+        runs.append([t.view(torch.uint8).cpu() for of in (w, m, v, c, s or []) for t in of])
+        before = [t.clone() for t in runs[-1]]
+        for k in range(5 if s else 4):
+            two = [[of[0], of[0].clone()] for of in (w, m, v, c, s or [torch.zeros(1)])]
+            two[k][1] = two[k][0]
+            with pytest.raises(bsp.BspError):
+                bsp.bsp_adamw_step(two[0], [G[0], G[0]], two[1], two[2], 1e-3, scales=two[4] if s else None, copies=two[3], **HYPER)
+        with pytest.raises(bsp.BspError):
+            bsp.bsp_adamw_step([w[0]], [G[0]], [m[0]], [m[0]], 1e-3, scales=[s[0]] if s else None, **HYPER)   # both moments one tensor
+        assert all(torch.equal(a, t.view(torch.uint8).cpu()) for a, t in zip(before, [t for of in (w, m, v, c, s or []) for t in of]))
+    assert all(torch.equal(a, b) for a, b in zip(runs[0], runs[1])) and all(torch.equal(a, b) for a, b in zip(runs[0], runs[2]))

@@ -208,3 +208,26 @@ def test_quantisation_of_a_few_very_long_rows_is_refused():
             assert q(P, 1, rows, cols, bsp.FP8_BLOCK, P, P, P, P, None) == SHAPE
             assert q(P, 1, rows, cols, bsp.FP8_ROW, None, None, P, P, None) == SHAPE
     assert q(P, 1, 33, 1 << 30, bsp.FP8_ROW, P, P, None, None, None) == SHAPE and q(P, 1, 1, (1 << 31) - 1, bsp.FP8_ROW, P, P, None, None, None) == SHAPE
+
+
+def test_adamw_refuses_results_that_share_memory():
+    """Whatever the step writes (weights, moments, scales, copies), of one tensor or of two: another workgroup would write the same place at the same time.
+    The calls that are refused for it are good ones with one address moved; gradients, masks and factors may be shared."""
+    L = bsp.lib()
+    n, kinds = 4 * 512, ("w", "m", "v", "scales", "copy")
+    size = {32: dict(w=4 * n, m=4 * n, v=4 * n, copy=2 * n), 8: dict(w=4 * n, m=n, v=n, scales=2 * (n // 256) * 4, copy=2 * n)}
+
+    def step(bits, places, **more):
+        each = [_Tensor(**dict(dict(g=1 << 30, keep=1 << 31, alpha=1 << 32, M=4, N=512, R=2), **p)) for p in places]
+        args = dict(dict(gdt=0, cdt=1, t=1), **more)
+        return L.bsp_adamw_step((_Tensor * len(each))(*each), len(each), args["gdt"], args["cdt"], bits, 0.0, 1e-3, 0.9, 0.999, 1e-8, args["t"], 0, None, None,
+                                None)
+    for bits in (32, 8):
+        for order in (1, -1):                    # in ascending order of their addresses and not
+            base = [{k: 1 << 20 | i << 16 | j << 22 for j, k in enumerate(kinds) if k in size[bits]} for i in range(3)][::order]
+            for i, a in ((i, a) for i in range(3) for a in size[bits]):
+                for o, b in ((o, b) for o in range(3) for b in size[bits] if (o, b) != (i, a)):
+                    for shift in (0, 4 - size[bits][a], size[bits][b] - 4):
+                        moved = [dict(p) for p in base]
+                        moved[i][a] = base[o][b] + shift
+                        assert step(bits, moved) == SHAPE, (bits, order, a, b, shift)
