@@ -478,6 +478,9 @@ int bsp_fp8_quant(const void *X, int xdt, int64_t rows, int64_t cols, int layout
 size_t bsp_matmul_fp8_workspace_bytes(int64_t T, int64_t M, int64_t K);
 int bsp_matmul_fp8(const void *A, const uint8_t *SA, const void *B, const uint8_t *SB, int b_layout, int64_t T, int64_t M, int64_t K,
                    const void *bias, int act, const void *residual, void *Y, int ydt, void *ws, size_t ws_bytes, void *stream);
+/* Which form a product of these sizes takes, host only: the side of its square tiles in tokens and outputs (0: up to 32 tokens in one pass over B), the
+ * steps of 128 columns that it keeps in LDS, and into how many runs the columns are split where there is scratch. */
+int bsp_matmul_fp8_form(int64_t T, int64_t M, int64_t K, int ydt, int act, int32_t *side, int32_t *depth, int32_t *splits);
 size_t bsp_linear_fp8_workspace_bytes(int64_t T, int64_t M, int64_t N);
 int bsp_linear_fp8(const void *X, int xdt, int64_t T, int64_t M, int64_t N, const void *W, const uint8_t *SW, int w_layout,
                    const void *bias, int act, const void *residual, void *Y, void *ws, size_t ws_bytes, void *stream);

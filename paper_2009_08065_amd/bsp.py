@@ -95,6 +95,7 @@ def lib():
     L.bsp_matmul_fp8_workspace_bytes.argtypes = [i64, i64, i64]
     L.bsp_matmul_fp8_workspace_bytes.restype = sz
     L.bsp_matmul_fp8.argtypes = [vp, vp, vp, vp, C.c_int, i64, i64, i64, vp, C.c_int, vp, vp, C.c_int, vp, sz, vp]
+    L.bsp_matmul_fp8_form.argtypes = [i64, i64, i64, C.c_int, C.c_int, vp, vp, vp]
     L.bsp_linear_fp8_workspace_bytes.argtypes = [i64, i64, i64]
     L.bsp_linear_fp8_workspace_bytes.restype = sz
     L.bsp_linear_fp8.argtypes = [vp, C.c_int, i64, i64, i64, vp, vp, C.c_int, vp, C.c_int, vp, vp, vp, sz, vp]
@@ -114,7 +115,7 @@ def lib():
     for name in ("bsp_group_norms", "bsp_penalty_grad", "bsp_prune_mask", "bsp_pack_count", "bsp_pack",
                  "bsp_packed_validate", "bsp_linear", "bsp_linear_ws", "bsp_linear_sized", "bsp_linear_transposed", "bsp_linear_transposed_ws", "bsp_linear_transposed_dense", "bsp_linear_dvals", "bsp_linear_plan", "bsp_linear_planned", "bsp_linear_planned_fused",
                  "bsp_mask_weights",
-                 "bsp_group_norms_grad", "bsp_adam_step", "bsp_prune_mask_count", "bsp_fp8_quant", "bsp_matmul_fp8", "bsp_linear_fp8", "bsp_block_norm",
+                 "bsp_group_norms_grad", "bsp_adam_step", "bsp_prune_mask_count", "bsp_fp8_quant", "bsp_matmul_fp8", "bsp_matmul_fp8_form", "bsp_linear_fp8", "bsp_block_norm",
                  "bsp_block_norm_backward", "bsp_adamw_step"):
         getattr(L, name).restype = C.c_int
     _LIB = L

@@ -635,6 +635,16 @@ extern "C" int bsp_matmul_fp8(const void *A, const uint8_t *SA, const void *B, c
     return product(A, SA, B, SB, b_layout, T, M, K, bias, act, residual, Y, ydt, ws, ws_bytes, (hipStream_t)stream);
 }
 
+extern "C" int bsp_matmul_fp8_form(int64_t T, int64_t M, int64_t K, int ydt, int act, int32_t *side, int32_t *depth, int32_t *splits) {
+    if (int st = check_sizes(T, M, K, BSP_FP8_ROW, ydt, act)) return st;
+    if (!side || !depth || !splits) return BSP_ERR_NULL;
+    const Shape c = choose(T, M, steps_of(K), ydt == BSP_F32, act == BSP_ACT_GELU);
+    *side = (c.tile + 1) / 2 * 2;
+    *depth = c.tile == 0 ? 0 : c.tile == 127 ? 3 : c.tile == 63 ? 4 : 2;
+    *splits = c.splits;
+    return BSP_OK;
+}
+
 extern "C" size_t bsp_linear_fp8_workspace_bytes(int64_t T, int64_t M, int64_t N) {
     if (T <= 0 || check_sizes(T, M, N, BSP_FP8_ROW, BSP_F32, BSP_ACT_NONE)) return 0;
     if (quantised_inside(T, steps_of(N))) return 0;

@@ -231,3 +231,15 @@ def test_adamw_refuses_results_that_share_memory():
                         moved = [dict(p) for p in base]
                         moved[i][a] = base[o][b] + shift
                         assert step(bits, moved) == SHAPE, (bits, order, a, b, shift)
+
+
+def test_form_of_a_product():
+    """The query knows what the call would refuse, and that few tokens have no tiles and few outputs of many columns are split where there is scratch."""
+    form = bsp.lib().bsp_matmul_fp8_form
+    v = [C.c_int32(-1) for _ in range(3)]
+    at = [C.byref(x) for x in v]
+    assert form(4, 8, 128, 5, 0, *at) == DTYPE and form(4, 8, 128, 1, 2, *at) == DTYPE and form(4, 0, 128, 1, 0, *at) == SHAPE and form(-1, 8, 128, 1, 0, *at) == SHAPE
+    assert form(4, 8, 128, 1, 0, None, at[1], at[2]) == NULL and form(4, 8, 128, 1, 0, at[0], at[1], None) == NULL and all(x.value == -1 for x in v)
+    for T in (0, 1, 32):
+        assert form(T, 4096, 1024, 1, 0, *at) == OK and [x.value for x in v] == [0, 0, 1]
+    assert form(100, 64, 8192, 0, 0, *at) == OK and v[0].value in (64, 128, 256) and v[1].value >= 2 and v[2].value > 1
