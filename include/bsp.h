@@ -450,7 +450,8 @@ int bsp_block_norm_backward(const void *dZ, const void *dH, const void *Z, const
  * bsp_fp8_quant: X [rows, cols] of xdt -> Q, S (codes and scales) and / or Qt, St: those of the transposed matrix, [cols, rp]
  * with segments along X's rows (BSP_FP8_ROW) or the same blocks (BSP_FP8_BLOCK).  The scale is the least power of two that
  * brings the segment's largest finite magnitude to 448 or below (2^0 for zeros, never below 2^-127); the code is the nearest
- * (ties to even).  What is not finite becomes NaN.  Q or Qt may be NULL; both 16-byte aligned.
+ * (ties to even), but never one whose value is beyond fp32's (a type's lowest value, as a mask, stays finite).  What is not finite
+ * becomes NaN.  Q or Qt may be NULL; both 16-byte aligned.
  *
  * bsp_matmul_fp8: Y = round(act(A B^T + bias) + residual) for quantised A [T, K] (BSP_FP8_ROW) and B [M, K] (b_layout):
  *   the layer          A = X,               B = W  (M x N, usually BSP_FP8_BLOCK)
@@ -458,7 +459,7 @@ int bsp_block_norm_backward(const void *dZ, const void *dH, const void *Z, const
  *   weight gradient    A = dY transposed,   B = X transposed (both BSP_FP8_ROW: segments along the tokens), ydt = BSP_F32
  * The matrix cores' sums are fp32, scaled exactly, and rounded once to ydt.  For 16-bit results the instruction on 8-bit codes is
  * used, which drops what lies 14 binades below the largest product of the few it adds at once (1.3e-5 of the result); for fp32
- * results one with exact products, at half the rate. bias [M] and
+ * results one with exact products of operands that it takes as bfloat16 (exact but for parts below 2^-133), at half the rate. bias [M] and
  * residual [T, M] have type ydt and may be NULL, act is a bsp_activation.  Y: [T, M].  The order of the additions is fixed for
  * given arguments: two calls give the same bits.  Codes past K must be 0 in A and B (bsp_fp8_quant's are).
  * ws: scratch for products of few outputs and many columns, bsp_matmul_fp8_workspace_bytes(T, M, K) bytes (may be 0), 256-byte

@@ -61,22 +61,23 @@ __global__ __launch_bounds__(kThreads) void quant_rows_kernel(Quant a) {
     const int64_t strip = blockIdx.x / a.tiles_c, tc = blockIdx.x - strip * a.tiles_c;  // (along the rows first)
     const int64_t row0 = strip * (kRowsEach * 16) + (threadIdx.x >> 4), col0 = 128 * tc + c0;
     const int cols = a.cols - col0 > 8 ? 8 : (int)(a.cols - col0);
-    Piece<DT> v[kRowsEach];
+    Piece<DT> raw[kRowsEach];
 #pragma unroll
-    for (int i = 0; i < kRowsEach; ++i) v[i].load(a.X, (row0 + 16 * i) * a.cols + col0, row0 + 16 * i < a.rows ? cols : 0);
+    for (int i = 0; i < kRowsEach; ++i) raw[i].load(a.X, (row0 + 16 * i) * a.cols + col0, row0 + 16 * i < a.rows ? cols : 0);
 #pragma unroll
     for (int i = 0; i < kRowsEach; ++i) {
         const int64_t row = row0 + 16 * i;
-        float m = 0.0f;
+        float v[8], m = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) m = __builtin_fmaxf(m, magnitude(v[i][j]));
+        for (int j = 0; j < 8; ++j) v[j] = raw[i][j], m = __builtin_fmaxf(m, magnitude(v[j]));
+        if (DT != BSP_F16) keep_below<8>(v, m);
         m = max_of_16(m);
         if (row >= a.rows) continue;
         const uint32_t e = scale_exponent(m);
         const float s = inverse_scale(e);
         float y[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = s * v[i][j];
+        for (int j = 0; j < 8; ++j) y[j] = s * v[j];
         *reinterpret_cast<uint2 *>(a.Q + row * a.pitch + col0) = make_uint2(codes4(y), codes4(y + 4));
         if ((threadIdx.x & 15) == 0) a.S[row * a.tiles_c + tc] = (uint8_t)e;
     }
@@ -96,10 +97,16 @@ __global__ __launch_bounds__(kTileThreads) void quant_kernel(Quant a) {
     const int64_t row0 = 128 * tr + r0, col0 = 128 * tc + c0;
     const int rows = a.rows - row0 > kEach ? kEach : (int)(a.rows - row0), cols = a.cols - col0 > 8 ? 8 : (int)(a.cols - col0);  // (may be negative)
 
-    Piece<DT> v[kEach];
+    Piece<DT> raw[kEach];
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) v[i].load(a.X, (row0 + i) * a.cols + col0, i < rows ? cols : 0);
+    for (int i = 0; i < kEach; ++i) raw[i].load(a.X, (row0 + i) * a.cols + col0, i < rows ? cols : 0);
+    float v[kEach][8];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = raw[i][j];
 
+    float most = 0.0f;  // of this thread's magnitudes
     uint32_t e_row[kEach], e_col[8];  // biased exponents of the rows' and the columns' scales
     if constexpr (BLOCK) {
         float m = 0.0f;
@@ -107,6 +114,7 @@ __global__ __launch_bounds__(kTileThreads) void quant_kernel(Quant a) {
         for (int i = 0; i < kEach; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) m = __builtin_fmaxf(m, magnitude(v[i][j]));
+        most = m;
         m = max_of_16(m);
         m = __builtin_fmaxf(m, __shfl_xor(m, 16));
         m = __builtin_fmaxf(m, __shfl_xor(m, 32));
@@ -129,6 +137,7 @@ __global__ __launch_bounds__(kTileThreads) void quant_kernel(Quant a) {
             float m = 0.0f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) m = __builtin_fmaxf(m, magnitude(v[i][j]));
+            most = __builtin_fmaxf(most, m);
             m = max_of_16(m);
             e_row[i] = scale_exponent(m);
             if (a.Q && (tid & 15) == 0 && i < rows) a.S[(row0 + i) * a.tiles_c + tc] = (uint8_t)e_row[i];
@@ -158,6 +167,10 @@ __global__ __launch_bounds__(kTileThreads) void quant_kernel(Quant a) {
         }
     }
 
+    if (DT != BSP_F16) {  // (the scales are the same)
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) keep_below<8>(v[i], most);
+    }
     if (a.Q) {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {

@@ -29,6 +29,19 @@ __device__ __forceinline__ uint32_t scale_exponent(float largest) {
 // 2^-e for a biased exponent of 0 to 253: exact, and so is a product with it unless the result is far below e4m3's least value.
 __device__ __forceinline__ float inverse_scale(uint32_t e) { return __uint_as_float((254u - e) << 23); }
 
+// From 1.9375 2^127 on (a type's lowest value, as a mask, is there) a value would go to the code 256 under the scale 2^120, and 2^128 is no number of fp32: it goes to 240,
+// where 1.875 2^127 goes, under the same scale.  A thread whose largest magnitude says that it has such values puts that one in their place; for the others it
+// is a comparison (8192 x 4096 in bf16 by rows 17.5 us as without; with every code held at or below a limit the kernels took up to 8 % longer).
+constexpr float kBeyond = 1.9375f * 0x1p127f;
+template <int N>
+__device__ __forceinline__ void keep_below(float *v, float largest) {
+    if (__builtin_expect(largest >= kBeyond, 0)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (magnitude(v[i]) >= kBeyond) v[i] = __builtin_copysignf(1.875f * 0x1p127f, v[i]);
+    }
+}
+
 // Four values of at most 448 as codes, to the nearest (ties to even); NaN for what is not finite.
 __device__ __forceinline__ uint32_t codes4(const float *y) {
     float x[4];

@@ -47,7 +47,7 @@ __device__ __forceinline__ f32x16 mfma_scaled(i32x8 a, i32x8 b, f32x16 c, uint32
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, (int)sa, 0, (int)sb);
 }
 
-// Eight codes times their scale as bfloat16 (exact).
+// Eight codes times their scale as bfloat16: exact for what is a whole multiple of 2^-133, its least number (only scales below 2^-124 have codes that are none).
 __device__ __forceinline__ uint4 widen8(uint32_t lo, uint32_t hi, uint32_t scale) {
     const float f = __uint_as_float(scale << 23);  // (the conversion takes the exponent: 0 is 2^-127)
     return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, f, false)),
@@ -361,6 +361,7 @@ __device__ __forceinline__ i32x8 quantise_segment(const void *X, int64_t at, int
     float m = 0.0f;
 #pragma unroll
     for (int k = 0; k < 32; ++k) m = __builtin_fmaxf(m, magnitude(v[k]));
+    if (XDT != BSP_F16) keep_below<32>(v, m);
     m = __builtin_fmaxf(m, __shfl_xor(m, 16));
     m = __builtin_fmaxf(m, __shfl_xor(m, 32));
     e = scale_exponent(m);

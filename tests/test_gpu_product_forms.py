@@ -14,6 +14,7 @@ pytestmark = pytest.mark.gpu
 DT = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
 TAG = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 D = torch.float64
+U = ob.U
 
 
 def rand(seed, *shape, std=1.0, dt=torch.float32):
@@ -119,3 +120,50 @@ def test_forms_that_split_the_columns(K, dtype):
                 y = res.clone()
                 inside(bsp.bsp_matmul_fp8(A, B, bias, act=act, residual=y, Y=y), want, bound, f"T={T} M={M} splits={splits}")
     assert seen or K < 4096
+
+
+# ---- the ends of the range ----------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 16, 32, 40, 300])
+def test_a_mask_of_the_types_lowest_value_stays_finite(T, dtype):
+    """The least finite values as inputs: their codes stand for numbers of fp32, so that beside weights of 0 (pruned ones, or gradients of masked tokens) a product
+    is what the other columns give."""
+    dt, M, N = DT[dtype], 48, 300
+    x, w = rand(1, T, N, dt=dt), rand(2, M, N, std=0.05, dt=dt)
+    low = torch.finfo(dt).min
+    x[:, 7], x[:, 8], x[0, 130] = low, -low, low
+    x[:, 9], x[:, 10] = 1.9374 * 2.0 ** 127, 1.9376 * 2.0 ** 127   # to the two sides of 248 of the scale (bf16: 1.9375 itself, a tie)
+    w[:, 7:11], w[:, 130] = 0, 0
+    for layout in (bsp.FP8_ROW, bsp.FP8_BLOCK):
+        X, Xt = bsp.bsp_fp8_quant(x, layout, want=("plain", "transposed"))
+        W = bsp.bsp_fp8_quant(w, layout)[0]
+        for q, cols in ((X, slice(7, 11)), (Xt, None)):
+            c = (q.codes.view(torch.uint8)[:, cols] if cols else q.codes.view(torch.uint8)[7:11].t()[:T]) & 127
+            assert (c == 0x77).all() and q.codes.float().isfinite().all()
+        assert (X.scales.max() == 247) and held(X).abs().max() == 240 * 2.0 ** 120
+        if layout == bsp.FP8_ROW:
+            xv, wv = held(X), held(W)
+            want = xv @ wv.t()
+            assert want.abs().max() < 1e3
+            y = bsp.bsp_matmul_fp8(X, W, out_dtype=torch.float32)
+            assert y.isfinite().all() and torch.equal(bsp.bsp_linear_fp8(x, W), bsp.bsp_matmul_fp8(X, W, out_dtype=dt))
+            inside(y, want, (N + 8) * U * (xv.abs() * (xv.abs() < 1e30)) @ wv.abs().t() + 1e-30)
+            # the gradient of the weights, where the masked tokens' gradients are zero
+            dy = rand(3, T, M, dt=dt)
+            dy[0] = 0
+            only = rand(4, T, N, dt=dt)
+            only[0] = low
+            D8, O8 = (bsp.bsp_fp8_quant(t, want=("transposed",))[1] for t in (dy, only))
+            assert bsp.bsp_matmul_fp8(D8, O8, out_dtype=torch.float32).isfinite().all()
+
+
+@pytest.mark.parametrize("T", [1, 40])
+def test_values_of_fp32_results_far_below(T):
+    """fp32 results have their operands as bfloat16: exact while they are whole multiples of 2^-133, and of those below it what is whole."""
+    M, K = 24, 128
+    for e in (-100, -118, -124, -130):
+        a, b = torch.zeros(T, K, device="cuda"), torch.zeros(M, K, device="cuda")
+        a[:, 0], a[:, 1] = 1.75 * 2.0 ** e, 1.5 * 2.0 ** (e - 1)
+        b[:, 0], b[:, 1] = 2.0 ** 60, 2.0 ** 62
+        y = bsp.bsp_matmul_fp8(bsp.bsp_fp8_quant(a)[0], bsp.bsp_fp8_quant(b)[0], out_dtype=torch.float32)
+        assert torch.equal(y, torch.full_like(y, 1.75 * 2.0 ** (e + 60) + 1.5 * 2.0 ** (e + 61))), e
