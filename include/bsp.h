@@ -458,8 +458,9 @@ int bsp_block_norm_backward(const void *dZ, const void *dH, const void *Z, const
  *   input gradient     A = dY,              B = the transposed W of the same call of bsp_fp8_quant
  *   weight gradient    A = dY transposed,   B = X transposed (both BSP_FP8_ROW: segments along the tokens), ydt = BSP_F32
  * The matrix cores' sums are fp32, scaled exactly, and rounded once to ydt.  For 16-bit results the instruction on 8-bit codes is
- * used, which drops what lies 14 binades below the largest product of the few it adds at once (1.3e-5 of the result); for fp32
- * results one with exact products of operands that it takes as bfloat16 (exact but for parts below 2^-133), at half the rate. bias [M] and
+ * used, which drops what lies 14 binades below the largest product of the eight columns that it adds at once: 1.3e-5 of the result where products do
+ * not cancel; where they do, as much of the largest products, whatever is left of them.  fp32 results come from an instruction with exact products of
+ * operands taken as bfloat16 (exact but for parts below 2^-133), at half the rate: the choice for products that cancel.  bias [M] and
  * residual [T, M] have type ydt and may be NULL, act is a bsp_activation.  Y: [T, M].  The order of the additions is fixed for
  * given arguments: two calls give the same bits.  Codes past K must be 0 in A and B (bsp_fp8_quant's are).
  * ws: scratch for products of few outputs and many columns, bsp_matmul_fp8_workspace_bytes(T, M, K) bytes (may be 0), 256-byte

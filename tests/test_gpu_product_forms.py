@@ -167,3 +167,29 @@ def test_values_of_fp32_results_far_below(T):
         b[:, 0], b[:, 1] = 2.0 ** 60, 2.0 ** 62
         y = bsp.bsp_matmul_fp8(bsp.bsp_fp8_quant(a)[0], bsp.bsp_fp8_quant(b)[0], out_dtype=torch.float32)
         assert torch.equal(y, torch.full_like(y, 1.75 * 2.0 ** (e + 60) + 1.5 * 2.0 ** (e + 61))), e
+
+
+# ---- products that cancel -----------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T", [1, 20, 40, 300])
+def test_products_that_cancel(T, dtype):
+    """Columns in pairs of opposite sign, one small product left in each output, away from the pairs and among them: fp32 results have it to the last bits
+    of the sum's magnitude; of 16-bit results what is off goes by the largest products of eight columns, not by the result."""
+    dt, M, K = DT[dtype], 72, 520
+    a, b = torch.zeros(T, K, device="cuda"), torch.zeros(M, K, device="cuda")
+    big, w = rand(1, T, 250), rand(2, M, 250)
+    a[:, 0:500:2], a[:, 1:500:2] = big, -big
+    b[:, 0:500:2], b[:, 1:500:2] = w, w
+    a[:, 510], b[:, 510] = 2.0 ** -5, 2.0 ** -4     # codes under the segments' scales; columns 504 to 511 hold nothing else
+    A, B = bsp.bsp_fp8_quant(a)[0], bsp.bsp_fp8_quant(b)[0]
+    av, bv = held(A), held(B)
+    want = av @ bv.t()
+    assert torch.equal(want, torch.full_like(want, 2.0 ** -9))
+    y = bsp.bsp_matmul_fp8(A, B, out_dtype=dt)
+    inside(y, want, ob.rounded_to(dt, want, ob.product(av, bv, dt)))
+    a[:, 510] = 0.0
+    a[:, 3], b[:, 3] = a[:, 3] + 2.0 ** -3, b[:, 3]  # now the rest of a pair
+    A, B = bsp.bsp_fp8_quant(a)[0], bsp.bsp_fp8_quant(b)[0]
+    av, bv = held(A), held(B)
+    want = av @ bv.t()
+    inside(bsp.bsp_matmul_fp8(A, B, out_dtype=dt), want, ob.rounded_to(dt, want, ob.product(av, bv, dt)))
