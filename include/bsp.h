@@ -171,7 +171,7 @@ int bsp_adam_step(float *W, const void *G, int gdt, float *m, float *v, int64_t 
 
 /* ---- one weight update of all tensors of a model (Alg. 2's "update W ... using Adam" for whole networks, with
  * decoupled weight decay) ------------------------------------------------------------------------
- * For every element of every tensor, fp32, one rounding per operation; g in gdt, the master weights w fp32:
+ * For every element of every tensor, in fp32 (state_bits 32: in this order, one rounding per operation); g in gdt, the master weights w fp32:
  *   g <- grad_scale * g           if grad_scale != NULL (a device float, read by the kernels: a clipping factor; where
  *                                 it is not finite the whole step is skipped and every buffer keeps its bits)
  *   g <- fma(lambda * alpha, w, g) if the tensor has alpha: Eq. 3 with fixed factors, squared-norm form (bsp_adam_step)
@@ -189,7 +189,8 @@ int bsp_adam_step(float *W, const void *G, int gdt, float *m, float *v, int64_t 
  *   element's index in its tensor, t and seed: equal calls give equal bits.  r > 0 is stored as the least positive code at
  *   least; a block whose largest value is below 2^-100 as zeros.  A block in which a moment is not finite (a gradient that was
  *   not, or whose square has no fp32 number) gets scales of 0: its elements start afresh.  The update itself uses the moments
- *   before they are stored.  All-zero codes and scales are a fresh state.
+ *   before they are stored, r in the place of sqrt(v), as w - ((lr/c1) * m) * (1 / fma(r, 1/sqrt(c2), eps)) with the hardware's reciprocal: from equal
+ *   moments that is within 15 * 2^-24 of state_bits 32's update, not bit for bit the same.  All-zero codes and scales are a fresh state.
  * tensors: HOST array of `count` descriptions, read during the call; device pointers in it.  Tensors are [M, N] row-major and
  *   contiguous (a vector: M = 1), of any size, 0 included; keep and alpha are [M / R, N], R is read only with them.
  *   What a call writes (weights, moments, scales, copies) may not overlap (it is refused: a tied tensor listed twice, say), nor
@@ -197,9 +198,8 @@ int bsp_adam_step(float *W, const void *G, int gdt, float *m, float *v, int64_t 
  * lr_t: NULL, or two device floats {lr, t} that the kernels read in the place of the arguments: a step that was captured in
  *   a graph is replayed with new ones (t as a float, 1 or more: exact up to 2^24).  A captured step without it repeats its t, and its random bits.
  * Up to 40 tensors are one launch.  Errors: BSP_ERR_NULL, BSP_ERR_DTYPE (gdt; cdt other than bf16 / fp16),
- * BSP_ERR_SHAPE (state_bits, t < 1 without lr_t, negative sizes, N >= 2^31, 2^34 elements or more, M % R != 0 with
- * keep or alpha, misalignment,
- * results that overlap), BSP_ERR_CAPACITY (no host memory for that check). */
+ * BSP_ERR_SHAPE (state_bits, t < 1 without lr_t, negative sizes, N >= 2^31, 2^34 elements or more (state_bits 8: 2^36),
+ * M % R != 0 with keep or alpha, misalignment, results that overlap), BSP_ERR_CAPACITY (no host memory for that check). */
 typedef struct {
     float *w;
     const void *g;

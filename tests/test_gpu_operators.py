@@ -841,3 +841,24 @@ def test_adamw_results_side_by_side_in_one_buffer(bits):
             bsp.bsp_adamw_step([w[0]], [G[0]], [m[0]], [m[0]], 1e-3, scales=[s[0]] if s else None, **HYPER)   # both moments one tensor
         assert all(torch.equal(a, t.view(torch.uint8).cpu()) for a, t in zip(before, [t for of in (w, m, v, c, s or []) for t in of]))
     assert all(torch.equal(a, b) for a, b in zip(runs[0], runs[1])) and all(torch.equal(a, b) for a, b in zip(runs[0], runs[2]))
+
+
+def test_adamw_8bit_update_from_equal_moments():
+    """The 8-bit form groups the update in its own way and divides with the hardware's reciprocal.  Its moments have the bits of the 32-bit step from the same
+    ones; then, in roundings of the update: 32 bits m / c1, the product with lr, half of v / c2, the root, the addition and the division, 5.5; 8 bits lr / c1,
+    r, 1 / sqrt(c2) (two), the fma, the reciprocal (1 ulp: two) and two products, 9: 15 together.  A step ends with one rounding of the weight's size in either."""
+    n = 4096
+    mc, vc = (orc.to_codes(rand(i, n, std=100.0).clamp(-448, 448).to(D)) for i in (1, 2))
+    vc = vc & 127
+    sc = (rand(3, 2, n // 256).abs() + 0.5) * 1e-6
+    each = sc.repeat_interleave(256, 1)
+    m32 = orc.from_codes(mc).float() * each[0]
+    r32 = orc.from_codes(vc).float() * each[1]
+    for t, lr, eps, decay in ((1, 1e-3, 1e-8, 0.0), (7, 2e-2, 1e-6, 0.01), (20000, 0.3, 1e-12, 0.0)):
+        hyper = dict(beta1=0.9, beta2=0.999, eps=eps, t=t, weight_decay=decay)
+        w0, g = rand(4, n, std=0.02), rand(5, n, std=1e-4)
+        a, b, none = w0.cuda(), w0.cuda(), torch.zeros(n, device="cuda")
+        bsp.bsp_adamw_step([a], [g.cuda()], [m32.cuda()], [(r32 * r32).cuda()], lr, **hyper)
+        bsp.bsp_adamw_step([none], [g.cuda()], [m32.cuda()], [(r32 * r32).cuda()], lr, **{**hyper, "weight_decay": 0.0})   # the update alone
+        bsp.bsp_adamw_step([b], [g.cuda()], [mc.cuda().view(torch.float8_e4m3fn)], [vc.cuda().view(torch.float8_e4m3fn)], lr, scales=[sc.cuda()], **hyper)
+        inside(b, a.cpu().to(D), 15 * U * none.cpu().to(D).abs() + 2 * U * a.cpu().to(D).abs() + 1e-38)
