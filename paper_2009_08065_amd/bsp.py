@@ -577,10 +577,11 @@ def bsp_fp8_quant(X, layout=FP8_ROW, want=("plain",)):
     return (None if Q is None else Fp8(Q, S, rows, cols, layout)), (None if Qt is None else Fp8(Qt, St, cols, rows, layout))
 
 
-def bsp_matmul_fp8(A: Fp8, B: Fp8, bias=None, act=0, residual=None, out_dtype=torch.bfloat16, Y=None):
-    """Y = round(act(A B^T + bias) + residual) of quantised A [T, K] (FP8_ROW) and B [M, K]."""
+def bsp_matmul_fp8(A: Fp8, B: Fp8, bias=None, act=0, residual=None, out_dtype=torch.bfloat16, Y=None, ws=None):
+    """Y = round(act(A B^T + bias) + residual) of quantised A [T, K] (FP8_ROW) and B [M, K].  ws: scratch of
+    bsp_matmul_fp8_workspace_bytes bytes (of no bytes: the columns are not split); without it the call allocates."""
     st, Y = _native().matmul_fp8(A.codes, A.scales, A.rows, A.cols, A.layout, B.codes, B.scales, B.rows, B.cols, B.layout, bias, act, residual,
-                                 _DT[out_dtype if Y is None else Y.dtype], Y, torch._C._cuda_getDevice(), _stream())
+                                 _DT[out_dtype if Y is None else Y.dtype], Y, ws, torch._C._cuda_getDevice(), _stream())
     _check(st, "bsp_matmul_fp8")
     return Y
 

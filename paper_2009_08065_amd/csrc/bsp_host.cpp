@@ -532,21 +532,21 @@ PyObject *fp8_quant(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     END_HANDLE_TH_ERRORS
 }
 
-// matmul_fp8(A's codes, scales, rows, cols, layout, B's, bias, act, residual, type, Y, device, stream) -> (status, Y); type: a bsp_dtype, of Y where that is None
+// matmul_fp8(A's codes, scales, rows, cols, layout, B's, bias, act, residual, type, Y, ws, device, stream) -> (status, Y); type: a bsp_dtype, of Y where that is None
 PyObject *matmul_fp8(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     HANDLE_TH_ERRORS
-    if (n_args != 17) {
-        PyErr_Format(PyExc_TypeError, "this function takes 17 arguments (%zd given)", n_args);
+    if (n_args != 18) {
+        PyErr_Format(PyExc_TypeError, "this function takes 18 arguments (%zd given)", n_args);
         return nullptr;
     }
     RowArgs a{"bsp_matmul_fp8", 0};
     Coded A, B;
-    const at::Tensor *bias, *residual, *Y;
+    const at::Tensor *bias, *residual, *Y, *ws;
     int act, type;
-    if (!read_whole(args[15], a.device) || !A.read(a, args) || !B.read(a, args + 5) || !a.take(args[10], bias) || !read_whole(args[11], act) ||
-        !a.take(args[12], residual) || !read_whole(args[13], type) || !a.take(args[14], Y))
+    if (!read_whole(args[16], a.device) || !A.read(a, args) || !B.read(a, args + 5) || !a.take(args[10], bias) || !read_whole(args[11], act) ||
+        !a.take(args[12], residual) || !read_whole(args[13], type) || !a.take(args[14], Y) || !a.take(args[15], ws))
         return nullptr;
-    void *stream = PyLong_AsVoidPtr(args[16]);
+    void *stream = PyLong_AsVoidPtr(args[17]);
     if (PyErr_Occurred()) return nullptr;
     if (A.layout != BSP_FP8_ROW || A.cols != B.cols) return a.fail("A must be quantised by rows and have the columns of B"), nullptr;
     constexpr at::ScalarType types[] = {at::kFloat, at::kBFloat16, at::kHalf};
@@ -563,10 +563,10 @@ PyObject *matmul_fp8(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
         const Unlocked unlocked;
         out = Y ? *Y : a.make({T, M}, types[type]);
         at::Tensor scratch;
-        size_t bytes = bsp_matmul_fp8_workspace_bytes(T, M, K);
-        if (bytes) scratch = a.make({(int64_t)bytes}, at::kByte);
+        const size_t bytes = ws ? (size_t)ws->nbytes() : bsp_matmul_fp8_workspace_bytes(T, M, K);
+        if (!ws && bytes) scratch = a.make({(int64_t)bytes}, at::kByte);
         st = bsp_matmul_fp8(A.codes->data_ptr(), (const uint8_t *)A.scales->data_ptr(), B.codes->data_ptr(), (const uint8_t *)B.scales->data_ptr(), B.layout,
-                            T, M, K, address(bias), act, address(residual), out.data_ptr(), type, bytes ? scratch.data_ptr() : nullptr, bytes, stream);
+                            T, M, K, address(bias), act, address(residual), out.data_ptr(), type, !bytes ? nullptr : ws ? ws->data_ptr() : scratch.data_ptr(), bytes, stream);
     }
     return with_status(st, &out, 1);
     END_HANDLE_TH_ERRORS

@@ -193,3 +193,25 @@ def test_products_that_cancel(T, dtype):
     av, bv = held(A), held(B)
     want = av @ bv.t()
     inside(bsp.bsp_matmul_fp8(A, B, out_dtype=dt), want, ob.rounded_to(dt, want, ob.product(av, bv, dt)))
+
+
+@pytest.mark.parametrize("T,M,K", [(100, 64, 8192), (200, 130, 4096), (300, 1000, 300), (5, 64, 1024)])
+def test_products_in_scratch_of_the_callers_own(T, M, K):
+    """The bits of the call that allocates, whatever the scratch holds before; without any bytes the columns are not split; too few are refused."""
+    A, B = bsp.bsp_fp8_quant(rand(1, T, K))[0], bsp.bsp_fp8_quant(rand(2, M, K))[0]
+    need = bsp.lib().bsp_matmul_fp8_workspace_bytes(T, M, K)
+    for dt in DT.values():
+        want = bsp.bsp_matmul_fp8(A, B, out_dtype=dt)
+        ws = torch.full((need + 64,), 255, dtype=torch.uint8, device="cuda")
+        for _ in range(2):
+            assert torch.equal(bsp.bsp_matmul_fp8(A, B, out_dtype=dt, ws=ws[:need] if need else ws), want)
+        assert (ws[need:] == 255).all()
+        av, bv = held(A), held(B)
+        s = av @ bv.t()
+        inside(bsp.bsp_matmul_fp8(A, B, out_dtype=dt, ws=ws[:0]), s, ob.rounded_to(dt, s, ob.product(av, bv, dt)))
+    if need:
+        with pytest.raises(bsp.BspError):
+            bsp.bsp_matmul_fp8(A, B, ws=ws[:need - 1])
+    for bad in (ws.cpu(), ws[::2], 3):
+        with pytest.raises((ValueError, TypeError)):
+            bsp.bsp_matmul_fp8(A, B, ws=bad)
