@@ -425,7 +425,8 @@ int bsp_linear_planned_fused(const void *X, int xdt, int64_t T, int64_t M, int64
  *   the same arguments give the same bits.  Arguments as in the forward call, Z as it wrote it; X is not needed, F for
  *   BSP_NORM_POST and dgate only, dH, Z and stats_pre for BSP_NORM_PRE only.  dX and dF may be dZ or dH (not each other).
  * ws: bsp_block_norm_backward_workspace_bytes(T, H, gate_rows) bytes (gate_rows 0 without a gate), 256-byte aligned,
- *   undefined before and after; calls that may overlap need one each.  Only needed where a sum down the rows is asked for.
+ *   undefined before and after; calls that may overlap need one each.  Only needed where a sum down the rows is asked for (room for all five kinds of
+ *   sums, whichever those are: 42 MB at H = 8192).
  * T == 0: nothing, and sums of zero (of up to 65531 gate rows).  Errors: BSP_ERR_NULL, BSP_ERR_DTYPE (dt, kind, norms), BSP_ERR_SHAPE (H outside 1 ..
  * 8192, T >= 2^31, gate_rows, a gradient of what is absent, misalignment), BSP_ERR_CAPACITY (ws_bytes). */
 typedef enum { BSP_NORM_LAYER = 0, BSP_NORM_RMS = 1 } bsp_norm_kind;
@@ -465,6 +466,9 @@ int bsp_block_norm_backward(const void *dZ, const void *dH, const void *Z, const
  * given arguments: two calls give the same bits.  Codes past K must be 0 in A and B (bsp_fp8_quant's are).
  * ws: scratch for products of few outputs and many columns, bsp_matmul_fp8_workspace_bytes(T, M, K) bytes (may be 0), 256-byte
  * aligned, undefined before and after; with NULL the call does without, slower.
+ *
+ * With a pruned matrix bsp_linear_planned, which reads and multiplies what is kept, is the faster one from a rate of about 2 on (up to 4 where M and N are 4096);
+ * these compute the dense product.
  *
  * bsp_linear_fp8: the layer on X [T, N] of type xdt and quantised W [M, N]: bsp_fp8_quant of X and bsp_matmul_fp8 in one call,
  * the same bits; bias, residual and Y have type xdt.  ws: bsp_linear_fp8_workspace_bytes(T, M, N) bytes (0 where few

@@ -8,8 +8,8 @@
 // between them (N_pre reads Z as it is stored, which is what the backward pass will see) cost no second look at memory.
 // A team is 16 lanes for the narrowest rows, one wavefront while a row has no more than 32 values for a lane (backward 16), else a workgroup.
 // Measured (MI355X, us, of a pass among others): forward 8192 x 1024 in bf16, BERT's form 14.3 (4.7 TB/s), both norms and a gate 16; in fp32 23.0 (5.8
-// TB/s); 16384 x 4096 in bf16 95 (5.6).  Backward 8192 x 1024, BERT's form 19.6 to 20.3 (16.9 and 3.9 for the columns; 4.2 TB/s), both norms and a gate 30; 16384 x
-// 4096 143 (4.7 TB/s) and 187.
+// TB/s); 16384 x 4096 in bf16 95 (5.6).  Backward 8192 x 1024, BERT's form 19.6 to 20.3 (16.9 and 3.9 for the columns; 4.2 TB/s), both norms and a gate 30 (3.4: its
+// vectors are asked for behind the first row sum, one row of a team is on its way at a time); 16384 x 4096 143 (4.7 TB/s) and 187 to 192 (4.2).
 // Sums are fp32: of a row by the lanes and then across them; the mean first, then the squares of what is left, which a
 // sum of squares less the square of the sum would lose where the mean is large.  The sums down the columns (gradients of w, b and gate) are kept
 // in registers over the rows of a workgroup, and a second launch adds the workgroups' sums in ascending order: equal calls give equal bits.

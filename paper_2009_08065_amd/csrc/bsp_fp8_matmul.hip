@@ -19,7 +19,7 @@
 // the operand reads of 16 lanes meet all banks.
 //
 // Measured (MI355X, us): 16384 x 4096, K = 4096 225 to 235 (2.4 PFLOP/s), 8192 x 4096, K = 1024 44 (1.6), with GELU 55, 8192 x 1024, K = 4096 37
-// (1.9); in fp32 4096 x 4096, K = 8192 200 (1.4 PFLOP/s), 1024 x 4096, K = 8192 67 (1.0); one token, 4096 x 1024 4.1 with its quantisation.
+// (1.9); in fp32 4096 x 4096, K = 8192 200 (1.4 PFLOP/s), 1024 x 4096, K = 8192 66 to 68 (1.0); one token, 4096 x 1024 4.1 with its quantisation.
 // What bounds the large ones: of 231 us in tiles of 256 x 256 182 are left without the loads (the matrix cores at the clock that their power leaves), 210
 // without the LDS reads; tiles of 128 x 128 fall from 266 to 162 without the loads, 16 TB/s of them.  Halves of steps in a ring of four, read into
 // registers ahead of the barrier, took 250, the first half of
@@ -156,11 +156,11 @@ __global__ __launch_bounds__(64 * WA * WB) void fp8_tile_kernel(Product p) {
         for (int j = 0; j < FB; ++j) o.b[j] = operand(cell_b, slot, j, sub);
     };
     // The products of half a step; after each of them `between` may put something else: a step's loads in a row would hold up the next product, on
-    // all wavefronts at once (fp32, 1024 x 4096, K = 8192 in tiles of 256: 160 us, dealt between the products 154).
+    // all wavefronts at once (fp32, 1024 x 4096, K = 8192 in tiles of 256: 4 % longer).
     constexpr int kProducts = FA * FB * (DT == BSP_F32 ? 4 : 1);
     auto multiply = [&](const Operands &o, auto between) {
         if constexpr (DT == BSP_F32) {
-            // (the next 16 columns are widened between the products of these: 1024 x 4096, K = 8192 72 us, 70)
+            // (the next 16 columns are widened between the products of these: 1024 x 4096, K = 8192 3 % shorter)
             uint4 wide[2][FA + FB];
             auto widen = [&](int to, int f, int k) {
                 const i32x8 &x = f < FA ? o.a[f] : o.b[f - FA];
@@ -502,7 +502,9 @@ double rounds_of(double n, double together, double alone) {
 // fills a compute unit, so that its epilogue (GELU: 8 us a round) hides nothing.  Two steps in LDS let two workgroups of 128 x 128 share a compute
 // unit and wait for each other; with three a workgroup that is alone on it reads half a step ahead.  Measured, 256 / 128 / 127 / 64 / 63: 16384 x
 // 4096, K = 4096 231 / 280 / 315 / 438 / 442; 8192 x 4096, K = 1024 44 / 44 / 62 / 66 / 82, with GELU 58 / 55 / 73 / 75 / 94; 2048 x 1024, K = 4096
-// 49 / 28 / 20 / 22 / 18; 512 x 1024, K = 4096 49 / 28 / 19 / 21 / 11; 1024 x 4096, K = 8192 in fp32 150 / 79 / 68 / 90 / 87.
+// 49 / 28 / 20 / 22 / 18; 512 x 1024, K = 4096 49 / 28 / 19 / 21 / 11; 1024 x 4096, K = 8192 in fp32 147 / 75 / 66 / 82 / 84.  The estimates are of rounds that fill the
+// chip: 4096 x 4096, K = 8192 in fp32 is one of 256 x 256 on all compute units and takes 199 (estimated 198); 64 or 128 such workgroups are faster, 147,
+// but there smaller tiles are faster still.
 double tile_us(int tile, double n, double steps, bool wide, bool gelu) {
     const double rounds = __builtin_ceil(n / 256.0);
     switch (tile) {
