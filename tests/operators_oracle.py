@@ -51,9 +51,7 @@ def quant(x, block):
     t = p.view(rp // h, h, cp // 128, 128)
     top = t.nan_to_num(0.0).abs().amax(dim=(1, 3))
     e = torch.tensor([[exponent(float(v)) for v in r] for r in top], dtype=torch.int64).view(top.shape)
-    y = torch.ldexp(t, (127 - e)[:, None, :, None].to(D))
-    y = torch.where((e == 247)[:, None, :, None] & (y.abs() > 240), torch.copysign(torch.full_like(y, 240.0), y), y)   # (256 2^120 is no number of fp32)
-    codes = to_codes(y.view(rp, cp))
+    codes = to_codes(torch.ldexp(t, (127 - e)[:, None, :, None].to(D)).view(rp, cp))
     return codes[:rows], (e if block else e[:rows]).to(torch.uint8)
 
 

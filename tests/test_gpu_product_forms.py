@@ -140,6 +140,8 @@ def test_a_mask_of_the_types_lowest_value_stays_finite(T, dtype):
         for q, cols in ((X, slice(7, 11)), (Xt, None)):
             c = (q.codes.view(torch.uint8)[:, cols] if cols else q.codes.view(torch.uint8)[7:11].t()[:T]) & 127
             assert (c == 0x77).all() and q.codes.float().isfinite().all()
+            codes, scales = ob.quant((x if cols else x.t()).cpu().to(D), layout == bsp.FP8_BLOCK)
+            assert torch.equal(q.codes.view(torch.uint8).cpu(), codes) and torch.equal(q.scales.cpu(), scales)
         assert (X.scales.max() == 247) and held(X).abs().max() == 240 * 2.0 ** 120
         if layout == bsp.FP8_ROW:
             xv, wv = held(X), held(W)
